@@ -79,15 +79,9 @@
 // same key permutation.
 #include <type_traits>
 
-#include "device_common.h"
+#include "attn_device.h"
 
 namespace sparstar {
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 // A step is sixteen MFMAs (and two barriers) at either head dim:
 // 32-key tiles at D = 128 (64-key tiles need more than 256 VGPRs in this
@@ -132,93 +126,6 @@ __device__ __forceinline__ int k_swz(int r) {
 template <class C>
 __device__ __forceinline__ int v_swz(int r) {
   return (((r / C::RPB) & 3) << 2) & (C::CPR - 1);
-}
-
-__device__ __forceinline__ float half_swap_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-
-__device__ __forceinline__ float half_swap_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
-}
-
-__device__ __forceinline__ s16x4 lds_read_tr(const uint16_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (__attribute__((address_space(3))) s16x4*)(const_cast<uint16_t*>(p)));
-}
-
-// Buffer descriptor as four dwords (raw buffer, stride 0, `bytes` records):
-// the form the inline-asm direct-to-LDS load takes.
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ i32x4 raw_rsrc(const void* base, uint32_t bytes) {
-  const uint64_t p = reinterpret_cast<uint64_t>(base);
-  i32x4 r;
-  r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)p);
-  r[1] = __builtin_amdgcn_readfirstlane((int)((uint32_t)(p >> 32) & 0xffffu));
-  r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
-  r[3] = 0x00020000;
-  return r;
-}
-
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-  return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
-}
-
-// Direct-to-LDS loads: lane l of a wave-wide load copies 16 bytes from
-// buffer offset voff (+ the instruction offset) to LDS byte m0 (+ the same
-// instruction offset) + 16 l.  Written as inline assembly so that the compiler
-// does not order every later LDS read behind them; each caller waits for these
-// loads explicitly (vmcnt) before a barrier makes the tile visible.
-//
-// A wave's share of one tile: N wave-wide loads after a single M0 write.  The
-// instruction offset moves the LDS destination and the memory address alike,
-// so load i goes to LDS m0 + 1024 i + 16 l and reads voff[i] + 1024 i (the
-// callers pass voff[i] already reduced by 1024 i).
-template <int N>
-__device__ __forceinline__ void dma_tile(uint32_t m0, const uint32_t* voff, i32x4 rsrc) {
-  static_assert(N == 1 || N == 2 || N == 4, "loads per wave and tile");
-  if constexpr (N == 1) {
-    asm volatile(
-        "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
-        "buffer_load_dwordx4 %1, %2, 0 offen lds"
-        :
-        : "s"(m0), "v"(voff[0]), "s"(rsrc)
-        : "memory", "m0");
-  } else if constexpr (N == 2) {
-    asm volatile(
-        "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
-        "buffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds"
-        :
-        : "s"(m0), "v"(voff[0]), "v"(voff[1]), "s"(rsrc)
-        : "memory", "m0");
-  } else {
-    asm volatile(
-        "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
-        "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
-        "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
-        "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds"
-        :
-        : "s"(m0), "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(rsrc)
-        : "memory", "m0");
-  }
-}
-
-// s_waitcnt with only the vector-memory counter constrained (<= n outstanding)
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-  static_assert(N >= 0 && N < 64, "vmcnt range");
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
 template <int D, int BLK, int NW, bool DENSE, bool SPLIT>
