@@ -316,6 +316,128 @@ int sparstar_token_topk_mass(const void* q, const void* k, int B, int H, int64_t
                              float softmax_scale, float* mass, void* workspace, size_t workspace_bytes,
                              void* stream);
 
+/*
+ * Bytes of device scratch the gradient calls below need: two fp32 values per query
+ * row, one bit per (key block, query block) pair, and, where a call of these sizes
+ * is cut into ranges, their fp32 partial results.  0 for invalid sizes.
+ */
+size_t sparstar_attn_bwd_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size);
+
+/*
+ * Gradients of sparstar_sparse_attn_fwd: with P the softmax weights of Eq. 7 over
+ * the listed blocks, recomputed from the forward's lse,
+ *   delta_t = sum_d dO_td O_td - dlse_t
+ *   dS_tu   = P_tu (dO_t . v_u - delta_t)
+ *   dV_u = sum_t P_tu dO_t,   dK_u = s sum_t dS_tu q_t,   dQ_t = s sum_u dS_tu k_u.
+ * Sums are held in fp32; P and dS are rounded to bf16 once, as operands of the
+ * products, and the results to bf16 once.  The call is deterministic.
+ *   q, k, v, B, H, Lq, Lk, D, block_size, softmax_scale   as for the forward
+ *   kv_num_blocks, kv_indices, kv_stride   the forward's lists.  (Malformed lists
+ *                   give unspecified values but no out-of-range access; an entry
+ *                   named twice in a row is one key block for dK and dV.)
+ *   o, lse          the forward's outputs, bf16 [B,H,Lq,D] and fp32 [B,H,Lq].  A row
+ *                   with lse = -inf (an empty list) has zero gradient and adds
+ *                   nothing to dK and dV.
+ *   d_o             device bf16 [B,H,Lq,D], the gradient of O
+ *   d_lse           device fp32 [B,H,Lq], the gradient of lse, or NULL for zero
+ *   dq, dk, dv      device bf16 out, the shapes of q, k and v; written whole (a key
+ *                   that no list names gets zeros).  They may not overlap the inputs.
+ *   workspace       device scratch of >= sparstar_attn_bwd_workspace_bytes(...)
+ *                   bytes, 256-byte aligned, no initialisation needed, garbage
+ *                   afterwards.  Calls that may overlap in time need one each.
+ * Lq == 0 writes zeros to dk and dv.  Heads that share keys and values: view Q (and
+ * O, lse and their gradients) of G such heads as one head of G Lq rows, [B, H / G,
+ * G Lq, D], in the forward and here (with lists: where Lq is a whole number of
+ * blocks); dK and dV then are the sums over the G heads.
+ */
+int sparstar_sparse_attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse,
+                             const void* d_o, const float* d_lse, int B, int H, int64_t Lq, int64_t Lk, int D,
+                             int block_size, const int32_t* kv_num_blocks, const int32_t* kv_indices, int kv_stride,
+                             float softmax_scale, void* dq, void* dk, void* dv, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Gradients of sparstar_dense_attn_fwd; arguments as for sparstar_sparse_attn_bwd. */
+int sparstar_dense_attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse,
+                            const void* d_o, const float* d_lse, int B, int H, int64_t Lq, int64_t Lk, int D,
+                            int block_size, float softmax_scale, void* dq, void* dk, void* dv, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The 8-bit key/value cache.  It holds, in the caller's buffers,
+ *   k_cache, v_cache   [B, H, cap, D] e4m3 codes (one byte each), 16-byte aligned
+ *   k_scale, v_scale   [B, H, ceil(cap / block_size)] bytes e + 127, one per block of
+ *                      tokens and head, e in [-117, 120]
+ * and a value is code * 2^e: exact in bf16, since a code has 4 significant bits.
+ *
+ * sparstar_cache_write appends L tokens: token i of batch element b becomes row
+ * start + i, or starts[b] + i.
+ *   k, v            device bf16 [B, H, L, D]
+ *   start           first row for every batch element (0 <= start, start + L <= cap)
+ *   starts          device int32 [B] or NULL: first row of each element instead of
+ *                   `start`.  Tokens that would land outside [0, cap) are dropped.
+ *   counts          device int32 [B] or NULL: only the element's first counts[b]
+ *                   tokens are written (clamped to [0, L]); a padded batch
+ * Per block, e is the least integer with amax * 2^-e <= 448 over its finite new
+ * values (e = -117 if they are all zero), and a code is the nearest e4m3 number,
+ * ties to even: off by at most 2^-4 of the value, or 2^(e-10) where the value is
+ * below 2^(e-6).  Infinities saturate at 448 * 2^e, NaN stays NaN.  Rows already in
+ * a block that the call continues (block start <= row < first new row) keep their
+ * values: e is at least theirs, and where it grows their codes are rounded to it.
+ * Rows behind the new ones count as empty: where a call ends inside a block, what
+ * that block held from there on loses its meaning, and its bytes stay as they are.
+ * No other block is touched.
+ */
+int sparstar_cache_write(const void* k, const void* v, int B, int H, int64_t L, int D, int block_size, int64_t start,
+                         const int32_t* starts, const int32_t* counts, int64_t cap, void* k_cache, void* v_cache,
+                         uint8_t* k_scale, uint8_t* v_scale, void* stream);
+
+/*
+ * Rows [start, start + L) of the cache as bf16 again, exactly: k and v [B, H, L, D],
+ * device bf16 out, 16-byte aligned, either of them NULL to leave it out.  For calls
+ * that take bf16 keys, such as sparstar_score_blocks.  0 <= start, start + L <= cap.
+ */
+int sparstar_cache_read(const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                        int B, int H, int64_t start, int64_t L, int64_t cap, int D, int block_size, void* k, void* v,
+                        void* stream);
+
+/*
+ * Bytes of device workspace that lets the calls below cut each list into ranges and
+ * join their partial results; 0 where these sizes are never cut, or invalid.
+ */
+size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size);
+
+/*
+ * sparstar_sparse_attn_fwd over the cache: query token t of block i attends to the
+ * rows u < len_b of the blocks on its list, with the values that the codes stand for.
+ * O and lse as there: bf16 queries, fp32 sums, P rounded to bf16 once.  Single tokens
+ * (Lq of 1 to 32) take a path of their own that streams the cache.
+ *   q, o            device bf16 [B,H,Lq,D];  lse device fp32 out [B,H,Lq], or NULL
+ *   k_cache .. v_scale, cap, block_size   the cache
+ *   Lk              rows in use, 1 <= Lk <= cap (the bound of every len_b)
+ *   lens            device int32 [B] or NULL: rows of each batch element, clamped to
+ *                   [0, Lk]; NULL: Lk.  Rows past it are never read.  An element
+ *                   without rows gets O = 0 and lse = -inf.
+ *   kv_num_blocks, kv_indices, kv_stride, softmax_scale   as for the bf16 forward;
+ *                   a listed block past len_b adds nothing
+ *   workspace       NULL for a single pass, or device scratch of at least
+ *                   sparstar_cache_attn_workspace_bytes(...) bytes, 256-byte aligned,
+ *                   no initialisation needed, garbage afterwards.  Calls that may
+ *                   overlap in time need one each.
+ * Heads that share keys and values: view Q of G such heads as [B, H / G, G Lq, D]
+ * (with lists: where Lq is a whole number of blocks, or where G Lq rows share one).
+ */
+int sparstar_cache_sparse_attn_fwd(const void* q, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
+                                   const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int64_t cap, int D,
+                                   int block_size, const int32_t* lens, const int32_t* kv_num_blocks,
+                                   const int32_t* kv_indices, int kv_stride, float softmax_scale, void* o, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same over all rows of the cache; arguments as there. */
+int sparstar_cache_dense_attn_fwd(const void* q, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
+                                  const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int64_t cap, int D,
+                                  int block_size, const int32_t* lens, float softmax_scale, void* o, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
 /* Message for the last non-OK return on this thread ("" if none). */
 const char* sparstar_last_error(void);
 

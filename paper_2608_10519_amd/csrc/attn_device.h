@@ -26,6 +26,14 @@ __device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
 }
 
+// B operand of 16-row k-step `half` of a 32-row sub-tile, of packed values
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bf16x8 pack_half(u32x8 pk, int half) {
+  const u32x4 lo = __builtin_shufflevector(pk, pk, 0, 1, 2, 3), hi = __builtin_shufflevector(pk, pk, 4, 5, 6, 7);
+  return __builtin_bit_cast(bf16x8, half == 0 ? lo : hi);
+}
+
 __device__ __forceinline__ s16x4 lds_read_tr(const uint16_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
       (__attribute__((address_space(3))) s16x4*)(const_cast<uint16_t*>(p)));

@@ -306,6 +306,12 @@ int score_blocks_internal(const void* q, const void* k, int B, int H, int64_t Lq
 
 int report_error(int code, const char* msg) { return fail(code, "%s", msg); }
 
+int clear_error() { return ok(); }
+
+int check_attn_sizes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size) {
+  return check_sizes(B, H, Lq, Lk, D, block_size);
+}
+
 size_t score_pooled_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size) {
   if (check_sizes(B, H, Lq, Lk, D, block_size) != SPARSTAR_OK) return 0;
   return ws_layout(B, H, Lq, Lk, D, block_size).s;

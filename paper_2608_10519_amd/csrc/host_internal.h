@@ -27,6 +27,13 @@ size_t score_pooled_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block
 // Sets the thread's last-error message and returns `code`.
 int report_error(int code, const char* msg);
 
+// Clears the message and returns SPARSTAR_OK.
+int clear_error();
+
+// The size checks that the attention calls share (SPARSTAR_OK, or a code with its
+// message set).
+int check_attn_sizes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size);
+
 }  // namespace sparstar
 
 // The cut of an attention call (attn_plan.h), for tests: key ranges, rotation,
@@ -34,3 +41,11 @@ int report_error(int code, const char* msg);
 // kv_stride 0 is the dense call.
 extern "C" void sparstar_internal_attn_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                             int64_t kv_stride, int with_workspace, int64_t out[5]);
+
+// The cut of a gradient call (bwd_plan.h): key ranges of the dQ pass, query ranges of the
+// dK/dV pass; and of an attention call over the cache (cache_plan.h): waves per
+// work-group, ranges.  For tests.  kv_stride 0 is the dense call.
+extern "C" void sparstar_internal_bwd_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size, int dense,
+                                           int64_t out[2]);
+extern "C" void sparstar_internal_cache_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                             int64_t kv_stride, int64_t out[2]);

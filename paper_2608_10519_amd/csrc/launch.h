@@ -141,6 +141,64 @@ struct TopkArgs {
   float scale;
 };
 
+// The attention's gradients (attn_bwd.hip).
+struct BwdArgs {
+  const uint16_t *q, *o, *d_o;   // [BH, Lq, D] bf16
+  const uint16_t *k, *v;         // [BH, Lk, D] bf16
+  const float* lse;              // [BH, Lq]
+  const float* dlse;             // [BH, Lq] or null
+  uint16_t* dq;                  // [BH, Lq, D]
+  uint16_t *dk, *dv;             // [BH, Lk, D]
+  const int32_t* kv_num_blocks;  // [BH, n_q] (sparse only)
+  const int32_t* kv_indices;     // [BH, n_q, stride] (sparse only)
+  int64_t lq, lk;
+  int bh, n_q, n_k, stride, block;
+  float scale, scale_log2;       // softmax scale, and times log2(e)
+  float* stats;                  // [BH, n_q * block / 32, 2, 32]: -lse log2(e), -delta
+  uint32_t* bits;                // [BH, n_k, n_words]: which query blocks list each key block (sparse only)
+  int n_words;                   // ceil(n_q / 32)
+  float* part;                   // fp32 partial results of the ranges: dQ, then dK and dV in the same place
+  int dq_ranges, dkv_ranges;     // ranges of each list's keys, and of the queries; 1: results go out at once
+};
+
+// The 8-bit key/value cache (cache.hip): e4m3 codes [BH, cap, D] and scale bytes
+// e + 127 [BH, ceil(cap / block)], value = code * 2^e.  The exponents' range keeps
+// every value a normal bf16 number: the smallest code is 2^-9.
+constexpr int kCacheExpMin = -117, kCacheExpMax = 120;
+
+struct CacheWriteArgs {
+  const uint16_t *k, *v;           // [BH, L, D] bf16
+  uint8_t *k_cache, *v_cache;      // [BH, cap, D]
+  uint8_t *k_scale, *v_scale;      // [BH, ceil(cap / block)]
+  const int32_t *starts, *counts;  // [B] or null: first row and number of the new tokens
+  int64_t l, cap, start;
+  int bh, heads;
+  int n_blocks;                    // blocks that L tokens can touch
+};
+
+struct CacheReadArgs {
+  const uint8_t *k_cache, *v_cache, *k_scale, *v_scale;
+  uint16_t *k_out, *v_out;         // [BH, L, D] bf16, either may be null
+  int64_t l, cap, start;
+  int bh, d, block;
+};
+
+struct CacheAttnArgs {
+  const uint16_t* q;               // [BH, Lq, D] bf16
+  const uint8_t *k_cache, *v_cache, *k_scale, *v_scale;
+  const int32_t* lens;             // [B] or null: tokens of each sequence
+  const int32_t* kv_num_blocks;    // [BH, n_q] (sparse only)
+  const int32_t* kv_indices;       // [BH, n_q, stride] (sparse only)
+  uint16_t* o;                     // [BH, Lq, D]
+  float* lse;                      // [BH, Lq] or null
+  int64_t lq, lk, cap;
+  int bh, heads, block, n_q, stride;
+  float scale_log2;
+  int ranges;                      // ranges of each list; 1: results go out at once
+  float* part_o;                   // [ranges, BH, Lq, D]: unnormalised P V
+  float* part_meta;                // [ranges, BH, Lq, 4]: running max (log2 units), row sums of the bf16 and the fp32 P
+};
+
 hipError_t launch_pool(const PoolArgs& a, int d, int block, hipStream_t stream);
 hipError_t launch_score(const ScoreArgs& a, int d, hipStream_t stream);
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
@@ -149,5 +207,9 @@ hipError_t launch_attn(const AttnArgs& a, int d, int block, bool dense, hipStrea
 hipError_t launch_retained_mass(const float* lse_sel, const float* lse_all, int64_t n, float* mass,
                                 hipStream_t stream);
 hipError_t launch_topk_mass(const TopkArgs& a, int d, hipStream_t stream);
+hipError_t launch_cache_write(const CacheWriteArgs& a, int d, int block, hipStream_t stream);
+hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, int d, int waves, bool dense, hipStream_t stream);
+hipError_t launch_attn_bwd(const BwdArgs& a, int d, bool dense, hipStream_t stream);
 
 }  // namespace sparstar

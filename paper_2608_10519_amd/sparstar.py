@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Sequence
+from typing import NamedTuple, Sequence
 
 import torch
 
@@ -75,6 +75,27 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.sparstar_token_topk_mass.argtypes = [c_p, c_p, c_i, c_i, c_i64, c_i64, c_i, ctypes.POINTER(ctypes.c_int64),
                                              c_i, c_p, c_p, c_f, c_p, c_p, c_sz, c_p]
     lib.sparstar_token_topk_mass.restype = c_i
+    lib.sparstar_attn_bwd_workspace_bytes.argtypes = [c_i, c_i, c_i64, c_i64, c_i, c_i]
+    lib.sparstar_attn_bwd_workspace_bytes.restype = c_sz
+    lib.sparstar_sparse_attn_bwd.argtypes = [c_p] * 7 + [c_i, c_i, c_i64, c_i64, c_i, c_i, c_p, c_p, c_i, c_f,
+                                                         c_p, c_p, c_p, c_p, c_sz, c_p]
+    lib.sparstar_sparse_attn_bwd.restype = c_i
+    lib.sparstar_dense_attn_bwd.argtypes = [c_p] * 7 + [c_i, c_i, c_i64, c_i64, c_i, c_i, c_f, c_p, c_p, c_p, c_p,
+                                                        c_sz, c_p]
+    lib.sparstar_dense_attn_bwd.restype = c_i
+    lib.sparstar_cache_write.argtypes = [c_p, c_p, c_i, c_i, c_i64, c_i, c_i, c_i64, c_p, c_p, c_i64, c_p, c_p, c_p,
+                                         c_p, c_p]
+    lib.sparstar_cache_write.restype = c_i
+    lib.sparstar_cache_read.argtypes = [c_p] * 4 + [c_i, c_i, c_i64, c_i64, c_i64, c_i, c_i, c_p, c_p, c_p]
+    lib.sparstar_cache_read.restype = c_i
+    lib.sparstar_cache_attn_workspace_bytes.argtypes = [c_i, c_i, c_i64, c_i64, c_i, c_i]
+    lib.sparstar_cache_attn_workspace_bytes.restype = c_sz
+    lib.sparstar_cache_sparse_attn_fwd.argtypes = [c_p] * 5 + [c_i, c_i, c_i64, c_i64, c_i64, c_i, c_i, c_p, c_p, c_p,
+                                                               c_i, c_f, c_p, c_p, c_p, c_sz, c_p]
+    lib.sparstar_cache_sparse_attn_fwd.restype = c_i
+    lib.sparstar_cache_dense_attn_fwd.argtypes = [c_p] * 5 + [c_i, c_i, c_i64, c_i64, c_i64, c_i, c_i, c_p, c_f, c_p,
+                                                              c_p, c_p, c_sz, c_p]
+    lib.sparstar_cache_dense_attn_fwd.restype = c_i
     lib.sparstar_last_error.argtypes = []
     lib.sparstar_last_error.restype = ctypes.c_char_p
     lib.sparstar_clip_keep_ranges.argtypes = [c_i, Range, Range, c_rp, c_i]
@@ -325,3 +346,169 @@ def sparstar_token_topk_mass(q: torch.Tensor, k: torch.Tensor, rows: Sequence[in
                                          _stream())
     _check("sparstar_token_topk_mass", rc)
     return mass
+
+
+def _like(t: torch.Tensor | None, shape, dtype, name: str) -> int | None:
+    """Pointer of an optional contiguous GPU tensor of this shape and type."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the GPU of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _lists(num: torch.Tensor, idx: torch.Tensor, B: int, H: int, Lq: int, block_size: int) -> tuple[int, int, int]:
+    n_q = -(-Lq // block_size)
+    if idx.dim() != 4:
+        raise ValueError("kv_indices must be [B, H, n_q, kv_stride]")
+    return (_like(num, (B, H, n_q), torch.int32, "kv_num_blocks"),
+            _like(idx, (B, H, n_q, idx.shape[-1]), torch.int32, "kv_indices"), idx.shape[-1])
+
+
+def sparstar_attn_bwd_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int) -> int:
+    return int(load().sparstar_attn_bwd_workspace_bytes(B, H, Lq, Lk, D, block_size))
+
+
+def _attn_bwd(fn, q, k, v, o, lse, d_o, lists, block_size, softmax_scale, dlse, out, workspace):
+    B, H, Lq, D = _bhld(q, "q")
+    _, _, Lk, _ = _bhld(k, "k")
+    bf16 = torch.bfloat16
+    kp, vp = (_like(t, (B, H, Lk, D), bf16, n) for t, n in ((k, "k"), (v, "v")))
+    op, dop = (_like(t, (B, H, Lq, D), bf16, n) for t, n in ((o, "o"), (d_o, "d_o")))
+    lp, dlp = (_like(t, (B, H, Lq), torch.float32, n) for t, n in ((lse, "lse"), (dlse, "dlse")))
+    listed = _lists(*lists, B, H, Lq, block_size) if lists is not None else ()
+    dq, dk, dv = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)) if out is None else out
+    grads = [_like(t, s.shape, bf16, n) for t, s, n in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv"))]
+    if workspace is None:
+        need = sparstar_attn_bwd_workspace_bytes(B, H, Lq, Lk, D, block_size)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    rc = getattr(load(), fn)(q.data_ptr(), kp, vp, op, lp, dop, dlp, B, H, Lq, Lk, D, block_size, *listed,
+                             float(softmax_scale), *grads, workspace.data_ptr(),
+                             workspace.numel() * workspace.element_size(), _stream())
+    _check(fn, rc)
+    return dq, dk, dv
+
+
+def sparstar_sparse_attn_bwd(q, k, v, o, lse, d_o, kv_num_blocks, kv_indices, block_size: int,
+                             softmax_scale: float = 0.0, *, dlse: torch.Tensor | None = None, out=None,
+                             workspace: torch.Tensor | None = None):
+    """Gradients of the block-sparse forward: returns (dq, dk, dv) in bf16.
+
+    o and lse are the forward's outputs, d_o (and dlse, where lse is used too) their
+    gradients.  `out` takes the three results, `workspace` the scratch, where the
+    caller keeps them."""
+    return _attn_bwd("sparstar_sparse_attn_bwd", q, k, v, o, lse, d_o, (kv_num_blocks, kv_indices), block_size,
+                     softmax_scale, dlse, out, workspace)
+
+
+def sparstar_dense_attn_bwd(q, k, v, o, lse, d_o, block_size: int = 64, softmax_scale: float = 0.0, *,
+                            dlse: torch.Tensor | None = None, out=None, workspace: torch.Tensor | None = None):
+    """Gradients of the dense forward: returns (dq, dk, dv) in bf16."""
+    return _attn_bwd("sparstar_dense_attn_bwd", q, k, v, o, lse, d_o, None, block_size, softmax_scale, dlse, out,
+                     workspace)
+
+
+class KvCache(NamedTuple):
+    """Keys and values in 8 bits: e4m3 codes and one scale byte e + 127 per block of
+    tokens and head; a value is code * 2^e."""
+    k: torch.Tensor        # [B, H, cap, D] float8_e4m3fn
+    v: torch.Tensor
+    k_scale: torch.Tensor  # [B, H, ceil(cap / block_size)] uint8
+    v_scale: torch.Tensor
+    block_size: int
+
+    @classmethod
+    def empty(cls, B: int, H: int, cap: int, D: int, block_size: int, device="cuda") -> "KvCache":
+        """An empty cache (its buffers need no initialisation)."""
+        codes = [torch.empty((B, H, cap, D), dtype=torch.float8_e4m3fn, device=device) for _ in range(2)]
+        scales = [torch.empty((B, H, -(-cap // block_size)), dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*codes, *scales, block_size)
+
+
+def _cache(c: KvCache, B: int, H: int, D: int) -> tuple[int, list[int]]:
+    """(capacity, the four pointers) of a cache that fits B, H and D."""
+    if c.k.dim() != 4:
+        raise ValueError("the cache's k must be [B, H, cap, D]")
+    cap = c.k.shape[2]
+    scale = (B, H, -(-cap // c.block_size) if c.block_size > 0 else 0)
+    return cap, [_like(c.k, (B, H, cap, D), torch.float8_e4m3fn, "cache.k"),
+                 _like(c.v, (B, H, cap, D), torch.float8_e4m3fn, "cache.v"),
+                 _like(c.k_scale, scale, torch.uint8, "cache.k_scale"),
+                 _like(c.v_scale, scale, torch.uint8, "cache.v_scale")]
+
+
+def sparstar_cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, start: int = 0, *,
+                         starts: torch.Tensor | None = None, counts: torch.Tensor | None = None) -> None:
+    """Appends k and v [B, H, L, D] to the cache at row `start`, or at row starts[b] of
+    each batch element (int32 on the GPU); counts[b] limits how many of the element's
+    tokens are written."""
+    B, H, L, D = _bhld(k, "k")
+    vp = _like(v, k.shape, torch.bfloat16, "v")
+    cap, ptrs = _cache(cache, B, H, D)
+    sp, cp = (_like(t, (B,), torch.int32, n) for t, n in ((starts, "starts"), (counts, "counts")))
+    rc = load().sparstar_cache_write(k.data_ptr(), vp, B, H, L, D, cache.block_size, start, sp, cp, cap, *ptrs,
+                                     _stream())
+    _check("sparstar_cache_write", rc)
+
+
+def sparstar_cache_read(cache: KvCache, start: int, L: int, *, want=("k", "v"), out=None):
+    """Rows [start, start + L) of the cache in bf16, exactly: (k, v), each [B, H, L, D], or
+    None for one that `want` leaves out."""
+    B, H, _, D = cache.k.shape
+    cap, ptrs = _cache(cache, B, H, D)
+    if out is None:
+        out = [torch.empty((B, H, L, D), dtype=torch.bfloat16, device=cache.k.device) if n in want else None
+               for n in ("k", "v")]
+    kp, vp = (_like(t, (B, H, L, D), torch.bfloat16, n) for t, n in zip(out, ("k", "v")))
+    rc = load().sparstar_cache_read(*ptrs, B, H, start, L, cap, D, cache.block_size, kp, vp, _stream())
+    _check("sparstar_cache_read", rc)
+    return tuple(out)
+
+
+def sparstar_cache_attn_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int) -> int:
+    return int(load().sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, block_size))
+
+
+def _cache_attn(fn, q, cache, lists, Lk, softmax_scale, lens, out, lse, return_lse, split, workspace):
+    B, H, Lq, D = _bhld(q, "q")
+    cap, ptrs = _cache(cache, B, H, D)
+    Lk = cap if Lk is None else Lk
+    b = cache.block_size
+    lp = _like(lens, (B,), torch.int32, "lens")
+    listed = _lists(*lists, B, H, Lq, b) if lists is not None else ()
+    o = torch.empty_like(q) if out is None else out
+    if lse is None and return_lse:
+        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device)
+    op, lsep = _like(o, q.shape, torch.bfloat16, "out"), _like(lse, (B, H, Lq), torch.float32, "lse")
+    wp, wn = None, 0
+    if split:
+        if workspace is None:
+            need = sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, b)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        if workspace is not None:
+            wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = getattr(load(), fn)(q.data_ptr(), *ptrs, B, H, Lq, Lk, cap, D, b, lp, *listed, float(softmax_scale), op, lsep,
+                             wp, wn, _stream())
+    _check(fn, rc)
+    return o, lse
+
+
+def sparstar_cache_sparse_attn_fwd(q, cache: KvCache, kv_num_blocks, kv_indices, Lk: int | None = None,
+                                   softmax_scale: float = 0.0, *, lens: torch.Tensor | None = None,
+                                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                                   return_lse: bool = True, split: bool = True,
+                                   workspace: torch.Tensor | None = None):
+    """Block-sparse forward over the first Lk rows of the cache (all of it by default), or
+    the first lens[b] of each batch element: returns (O, lse).  split=False runs a single
+    pass without a workspace."""
+    return _cache_attn("sparstar_cache_sparse_attn_fwd", q, cache, (kv_num_blocks, kv_indices), Lk, softmax_scale,
+                       lens, out, lse, return_lse, split, workspace)
+
+
+def sparstar_cache_dense_attn_fwd(q, cache: KvCache, Lk: int | None = None, softmax_scale: float = 0.0, *,
+                                  lens: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                                  lse: torch.Tensor | None = None, return_lse: bool = True, split: bool = True,
+                                  workspace: torch.Tensor | None = None):
+    """Dense forward over the cache: returns (O, lse)."""
+    return _cache_attn("sparstar_cache_dense_attn_fwd", q, cache, None, Lk, softmax_scale, lens, out, lse, return_lse,
+                       split, workspace)
