@@ -380,7 +380,8 @@ int sparstar_dense_attn_bwd(const void* q, const void* k, const void* v, const v
  * Per block, e is the least integer with amax * 2^-e <= 448 over its finite new
  * values (e = -117 if they are all zero), and a code is the nearest e4m3 number,
  * ties to even: off by at most 2^-4 of the value, or 2^(e-10) where the value is
- * below 2^(e-6).  Infinities saturate at 448 * 2^e, NaN stays NaN.  Rows already in
+ * below 2^(e-6).  Infinities saturate at 448 * 2^e (what would exceed it, at 240 * 2^e,
+ * where e = 120, the last value below bf16's end), NaN stays NaN.  Rows already in
  * a block that the call continues (block start <= row < first new row) keep their
  * values: e is at least theirs, and where it grows their codes are rounded to it.
  * Rows behind the new ones count as empty: where a call ends inside a block, what

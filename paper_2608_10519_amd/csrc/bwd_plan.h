@@ -32,7 +32,7 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   p.dq_ranges = bwd_ranges(bh * ((lq + rows - 1) / rows), 256 * 8 / waves, (lk + tile - 1) / tile);
   p.dkv_ranges = bwd_ranges(bh * ((lk + rows - 1) / rows), 256 * (d == 128 ? 4 : 8) / waves, (lq + tile - 1) / tile);
   // (the sparse walk is cut at whole words of 32 query blocks)
-  if (!dense) p.dkv_ranges = (int)std::min<int64_t>(p.dkv_ranges, (nq + 31) / 32);
+  if (!dense) p.dkv_ranges = (int)std::min<int64_t>(p.dkv_ranges, std::max<int64_t>(1, (nq + 31) / 32));
   auto align = [](size_t x) { return (x + 255) & ~size_t(255); };
   p.stats = 0;
   p.bits = align(size_t(bh * nq * block) * 2 * sizeof(float));

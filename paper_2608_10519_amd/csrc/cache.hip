@@ -19,10 +19,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // 2^e of a scale byte: the byte is the exponent field of the float
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// four values -> four e4m3 codes (nearest even).  Infinities, the only values past 448
-// after scaling, saturate; NaN stays NaN.
-__device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d) {
-  auto sat = [](float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); };
+// four values -> four e4m3 codes (nearest even).  Infinities, and what would round past
+// `most`, saturate there; NaN stays NaN.
+__device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d, float most) {
+  auto sat = [most](float x) { return x != x ? x : fminf(fmaxf(x, -most), most); };
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), r, true);
 }
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
       for (int i = threadIdx.x; i < n; i += 256) {
         const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(old[i], 1.f, false);
         const bf16x2 q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(old[i], 1.f, true);
-        old[i] = pack4_e4m3((float)p[0] * f, (float)p[1] * f, (float)q[0] * f, (float)q[1] * f);
+        old[i] = pack4_e4m3((float)p[0] * f, (float)p[1] * f, (float)q[0] * f, (float)q[1] * f, 448.f);
       }
     } else {
       e = held;
@@ -99,6 +99,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
   }
   if (threadIdx.x == 0) *scale = (uint8_t)(e + 127);
   const float inv = __builtin_amdgcn_ldexpf(1.f, -e);
+  // (256 * 2^120 is past the largest bf16 number)
+  const float most = e == kCacheExpMax ? 240.f : 448.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int c = threadIdx.x + 256 * i;
@@ -106,8 +108,8 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
     if (row < first || row >= end) continue;
     const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
     uint2 r;
-    r.x = pack4_e4m3(bf16_lo(u[0]) * inv, bf16_hi(u[0]) * inv, bf16_lo(u[1]) * inv, bf16_hi(u[1]) * inv);
-    r.y = pack4_e4m3(bf16_lo(u[2]) * inv, bf16_hi(u[2]) * inv, bf16_lo(u[3]) * inv, bf16_hi(u[3]) * inv);
+    r.x = pack4_e4m3(bf16_lo(u[0]) * inv, bf16_hi(u[0]) * inv, bf16_lo(u[1]) * inv, bf16_hi(u[1]) * inv, most);
+    r.y = pack4_e4m3(bf16_lo(u[2]) * inv, bf16_hi(u[2]) * inv, bf16_lo(u[3]) * inv, bf16_hi(u[3]) * inv, most);
     *reinterpret_cast<uint2*>(codes + row * D + 8 * (c % CPR)) = r;
   }
 }
@@ -116,9 +118,10 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
   const int64_t cpr = a.d / 16, per_bh = a.l * cpr, n = (int64_t)a.bh * per_bh;
   int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  // the first n threads take K where it is wanted, the next n (or the first) V
   const bool is_v = a.k_out == nullptr || i >= n;
   if (a.k_out != nullptr && is_v) i -= n;
-  if (i >= n) return;
+  if (i >= n || (is_v && a.v_out == nullptr)) return;
   const int64_t bh = i / per_bh, r = i - bh * per_bh;
   const int64_t row = a.start + r / cpr;
   const uint8_t* codes = (is_v ? a.v_cache : a.k_cache) + (bh * a.cap + row) * a.d + 16 * (r % cpr);
