@@ -32,11 +32,16 @@ FLAGS = [
 # Every kernel must run without a private (scratch) segment: a register spill to
 # scratch memory is a build error, not a silent slowdown.
 DEVICE_FLAGS = ["-Xarch_device", "-Wframe-larger-than=0", "-Xarch_device", "-Werror=frame-larger-than"]
+# The gradient kernels hold more than 256 registers a wave.  Left alone the compiler then
+# keeps every matrix product in the upper half of the register file, and copies what the
+# softmax reads (32 values a step) down from there.
+SOURCE_FLAGS = {"attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD_DIR, os.path.basename(src) + ".o")
     lang = ["-x", "hip", *DEVICE_FLAGS] if src.endswith(".hip") else []
+    lang = lang + SOURCE_FLAGS.get(src, [])
     cmd = [HIPCC, *FLAGS, *lang, "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

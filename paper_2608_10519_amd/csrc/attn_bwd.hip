@@ -18,17 +18,19 @@
 //
 // The key groups find their query blocks in a bit matrix, one bit per (key block,
 // query block), that a small kernel builds from the lists.
+#include <type_traits>
+#include <utility>
+
 #include "attn_device.h"
 
 namespace sparstar {
 
-// Tiles are 8 KB: 32 rows at D = 128, 64 at D = 64.  Rows are stored unpadded in LDS
-// and their 16-byte chunks XOR-permuted by swz(row), which leaves both reads of a
+// Tiles of 32 or 64 rows.  Rows are stored unpadded in LDS and their 16-byte chunks XOR-permuted by swz(row), which leaves both reads of a
 // tile free of bank conflicts: 16 consecutive rows of one chunk (ds_read_b128), and
 // four consecutive rows of four chunks (the transpose read).
-template <int D>
+template <int D, int ROWS = attn_tile_keys(D)>
 struct BwdCfg {
-  static constexpr int KB = attn_tile_keys(D);  // rows per tile
+  static constexpr int KB = ROWS;               // rows per tile
   static constexpr int KT = KB / 32;            // 32-row sub-tiles
   static constexpr int DS = D / 16;             // MFMA k-steps over D
   static constexpr int DT = D / 32;             // 32-row tiles of a D-row result
@@ -37,7 +39,6 @@ struct BwdCfg {
   static constexpr int RPD = 1024 / RB;         // rows per direct-to-LDS wave load
   static constexpr int TILE = KB * D;           // elements per tile
   static constexpr int TILE_BYTES = TILE * 2;
-  static_assert(TILE_BYTES == 8192, "8 KB tiles");
 };
 
 template <int D>
@@ -92,11 +93,23 @@ __device__ __forceinline__ bf16x8 load_row(const uint16_t* p, bool ok) {
   return __builtin_bit_cast(bf16x8, u);
 }
 
-// The direct-to-LDS loads of one tile by NW waves.
-template <int D, int NW>
+// Which rows of a [rows, D] tensor a tile holds: tiles below `whole` lie inside it, tile
+// `whole` holds what is left, and later ones (and -1) hold nothing.
+template <class C>
+struct TileRows {
+  uint32_t whole, last_bytes;
+  __device__ __forceinline__ explicit TileRows(int64_t rows)
+      : whole((uint32_t)(rows / C::KB)), last_bytes((uint32_t)(rows % C::KB) * (uint32_t)C::RB) {}
+  __device__ __forceinline__ uint32_t bytes(int tile) const {
+    return (uint32_t)tile < whole ? (uint32_t)C::TILE_BYTES : ((uint32_t)tile == whole ? last_bytes : 0u);
+  }
+};
+
+// The direct-to-LDS loads of one tile by NW waves; rows that do not exist arrive as zeros.
+template <class C, int NW>
 struct TileLoad {
-  using C = BwdCfg<D>;
-  static constexpr int N = 8 / NW;  // 1 KB loads per wave
+  static constexpr int D = C::RB / 2;
+  static constexpr int N = C::TILE_BYTES / 1024 / NW;  // 1 KB loads per wave
   uint32_t off[N];
   __device__ __forceinline__ TileLoad(int wave, int lane) {
 #pragma unroll
@@ -106,19 +119,17 @@ struct TileLoad {
       off[i] = (uint32_t)(r * C::RB + 16 * ((lane % C::CPR) ^ bwd_swz<D>(r)) - 1024 * i);
     }
   }
-  // rows [row0, row0 + KB) of a [rows, D] tensor; rows past its end arrive as zeros
-  __device__ __forceinline__ void issue(const uint16_t* base, int64_t row0, int64_t rows, uint16_t* slot,
-                                        int wave) const {
-    int64_t left = rows - row0;
-    left = left < 0 ? 0 : (left > C::KB ? C::KB : left);
-    const i32x4 rs = raw_rsrc(base + row0 * D, (uint32_t)left * (uint32_t)C::RB);
+  // the tile's descriptor, and its loads
+  __device__ __forceinline__ static i32x4 rsrc(const uint16_t* base, int tile, uint32_t bytes) {
+    return raw_rsrc(base + (int64_t)tile * C::TILE, bytes);
+  }
+  __device__ __forceinline__ void issue(i32x4 rs, uint16_t* slot, int wave) const {
     dma_tile<N>(lds_addr(slot) + (uint32_t)(N * wave) * 1024u, off, rs);
   }
 };
 
 // 64 consecutive floats into LDS (lane l: 4 bytes at +4 l)
-__device__ __forceinline__ void dma_floats(const float* src, float* slot, int lane) {
-  const i32x4 rs = raw_rsrc(src, 256);
+__device__ __forceinline__ void dma_floats(i32x4 rs, float* slot, int lane) {
   const uint32_t voff = (uint32_t)lane * 4u;
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
@@ -129,8 +140,18 @@ __device__ __forceinline__ void dma_floats(const float* src, float* slot, int la
       : "memory", "m0");
 }
 
-// ---- per-row statistics.  Rows are kept in groups of 32, [32] of
-// -lse log2(e) then [32] of -delta, padded to whole query blocks: a row past Lq,
+// The barrier of a step: the tile that the wave waits for has landed and can be read by
+// all, and every wave is done with the tile that the loads after it overwrite.  (Its reads
+// were consumed by MFMAs long before: no wait for LDS is needed.)
+__device__ __forceinline__ void publish() {
+  wait_vmcnt<0>();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ---- per-row statistics.  Rows are kept in groups of 32, [32] of -lse / s (what an
+// unscaled logit is offset by) then [32] of -delta, padded to whole query blocks: a row past Lq,
 // and one that saw no key, gets -inf and 0, which makes its P and dS zero.
 template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(BwdArgs a) {
@@ -160,7 +181,7 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(BwdArgs a) {
     if (in) {
       const float l = a.lse[r];
       if (l != -INFINITY) {
-        nl = -l * 1.44269504088896340736f;
+        nl = -l * a.inv_scale;
         nd = (a.dlse != nullptr ? a.dlse[r] : 0.f) - sum;
       }
     }
@@ -197,16 +218,39 @@ __global__ __launch_bounds__(1024) void attn_bwd_bits_kernel(BwdArgs a) {
   for (int j = threadIdx.x; j < hi - lo; j += 1024) a.bits[(bh * a.n_k + lo + j) * a.n_words + word] = bits[j];
 }
 
+// f(0), .., f(N - 1) with each index a compile-time constant
+template <class F, int... I>
+__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for(f, std::make_integer_sequence<int, N>{});
+}
+
 // ---- dQ: one work-group per (head, list range, query group of 32 NW rows), one
-// wave per 32 rows.  Per 32-key sub-tile S^T = K Q^T and dP^T = V dO^T (lane: 16
-// keys of one query), then dQ^T += K^T dS^T with dS rounded to bf16 once.
+// wave per 32 rows.  Per 32-key tile S^T = K Q^T and dP^T = V dO^T (lane: 16 keys of
+// one query), then dQ^T += K^T dS^T with dS rounded to bf16 once.  The step is that of
+// the dK/dV pass below: S and dP of tile t + 1, then dQ of tile t, 24 MFMAs at D = 128.
+template <int D>
+struct DqCfg : BwdCfg<D, 32> {
+  using B = BwdCfg<D, 32>;
+  static constexpr int NA = 2 * B::DS, NB = 2 * B::DT, NM = NA + NB;  // MFMAs of a step
+  static constexpr int SPREAD = NA + B::DT - 1;    // MFMAs that the softmax is spread over
+  static constexpr int P = 4;                      // MFMAs between an operand's read and its use
+  static constexpr int RING = 4;                   // tiles in LDS, K and V each
+  // dP starts from -delta, held in 16 registers, where there are as many; else it is
+  // added per element
+  static constexpr bool START = D == 64;
+};
+
 template <int D, int NW, bool DENSE>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_bwd_dq_kernel(BwdArgs a) {
-  using C = BwdCfg<D>;
+  using C = DqCfg<D>;
   constexpr int ROWS = 32 * NW, SUB = ROWS / C::KB;  // (sparse: a list entry is SUB tiles)
-  __shared__ __attribute__((aligned(1024))) uint16_t ks[2][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t vs[2][C::TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t ks[C::RING][C::TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t vs[C::RING][C::TILE];
   const int64_t n_g = (a.lq + ROWS - 1) / ROWS;
   const int64_t w = xcd_linear(blockIdx.x, gridDim.x);
   const int64_t pair = w / n_g;
@@ -227,12 +271,18 @@ void attn_bwd_dq_kernel(BwdArgs a) {
       dof[s] = load_row(a.d_o + at + 16 * s, row_ok);
     }
   }
-  float nl = -INFINITY, nd = 0.f;
-  if (row_ok) {
-    const int64_t i = bh * a.n_q * a.block + row;
-    nl = a.stats[(i / 32) * 64 + i % 32];
-    nd = a.stats[(i / 32) * 64 + 32 + i % 32];
+  float nl = -INFINITY;
+  float nd = 0.f;
+  {
+    if (row_ok) {
+      const int64_t i = bh * a.n_q * a.block + row;
+      nl = a.stats[(i / 32) * 64 + i % 32] * a.scale_log2;
+      nd = a.stats[(i / 32) * 64 + 32 + i % 32];
+    }
   }
+  f32x16 start;  // where each dP of the lane's query starts from
+#pragma unroll
+  for (int e = 0; e < 16; ++e) start[e] = C::START ? nd : 0.f;
 
   // the range's entries of the list (or key tiles of the dense call)
   int first = 0, cnt;
@@ -261,6 +311,7 @@ void attn_bwd_dq_kernel(BwdArgs a) {
   };
   const int ntiles = DENSE ? cnt : cnt * SUB;
   auto fetch = [&](int j) -> int {
+    if (j >= ntiles) return -1;
     if constexpr (DENSE) {
       return first + j;
     } else {
@@ -271,13 +322,22 @@ void attn_bwd_dq_kernel(BwdArgs a) {
   };
 
   const BwdOffsets<D> off(lane);
-  const TileLoad<D, NW> load(wave, lane);
+  const TileLoad<C, NW> load(wave, lane);
   const uint16_t* const kbase = a.k + bh * a.lk * D;
   const uint16_t* const vbase = a.v + bh * a.lk * D;
+  const TileRows<C> rows(a.lk);
   auto issue = [&](int tile, int slot) {
-    const int64_t row0 = tile < 0 ? 0 : (int64_t)tile * C::KB, rows = tile < 0 ? 0 : a.lk;
-    load.issue(kbase, row0, rows, ks[slot], wave);
-    load.issue(vbase, row0, rows, vs[slot], wave);
+    load.issue(load.rsrc(kbase, tile, rows.bytes(tile)), ks[slot], wave);
+    load.issue(load.rsrc(vbase, tile, rows.bytes(tile)), vs[slot], wave);
+  };
+  // keys past Lk, and all of a tile that does not exist, are masked
+  auto mask_tile = [&](f32x16& x, int tile) {
+    const int64_t left = tile < 0 ? 0 : a.lk - (int64_t)tile * C::KB;
+    const int vis = (int)(left < 0 ? 0 : left) - 4 * hh;
+    asm volatile("; mask");  // (keeps the branch around this: it is rarely taken)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (8 * (e / 4) + e % 4 >= vis) x[e] = -INFINITY;
   };
   f32x16 acc[C::DT];
 #pragma unroll
@@ -286,52 +346,129 @@ void attn_bwd_dq_kernel(BwdArgs a) {
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
 
   if (ntiles > 0) {
+    // MFMA n < NA of a step: S (n even) or dP of tile t + 1; n >= NA: dQ of tile t
+    auto read_a = [&](int n, int slot) -> bf16x8 {
+      return tile_row<D>(n % 2 == 0 ? ks[slot] : vs[slot], off, 0, n / 2);
+    };
+    auto read_b = [&](int m, int slot) -> bf16x8 { return tile_col<D>(ks[slot], off, 0, m / C::DT, m % C::DT); };
     if constexpr (!DENSE) load_batch(0);
-    int tile = fetch(0);
-    issue(tile, 0);
-    for (int j = 0; j < ntiles; ++j) {
-      const int next = j + 1 < ntiles ? fetch(j + 1) : -1;
-      wait_vmcnt<0>();
-      __syncthreads();
-      if (j + 1 < ntiles) issue(next, (j + 1) & 1);
-      const uint16_t* kt_lds = ks[j & 1];
-      const uint16_t* vt_lds = vs[j & 1];
-      const int64_t left = tile < 0 ? 0 : a.lk - (int64_t)tile * C::KB;
+    int t0 = fetch(0), t1 = fetch(1), t2 = fetch(2);
+    issue(t0, 0);
+    issue(t1, 1);
+    issue(t2, 2);
+    wait_vmcnt<0>();
+    __syncthreads();
+    f32x16 s, dp = start;  // S and dP of tile t
 #pragma unroll
-      for (int kt = 0; kt < C::KT; ++kt) {
-        f32x16 s, dp;
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    static_for<C::NA>([&](auto nc) {
+      constexpr int n = decltype(nc)::value;
+      const bf16x8 x = read_a(n, 0);
+      if constexpr (n % 2 == 0) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[n / 2], s, 0, 0, 0);
+      else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, dof[n / 2], dp, 0, 0, 0);
+    });
+    if ((uint32_t)t0 >= rows.whole) mask_tile(s, t0);
+    bf16x8 ahead[C::P];  // operands of the next MFMAs
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          s[e] = 0.f;
-          dp[e] = nd;
+    for (int i = 0; i < C::P; ++i) ahead[i] = read_a(i, 1);
+
+    int j = 0;  // tile t is the walk's j-th
+    auto step = [&](auto tc) {
+      constexpr int T = decltype(tc)::value;  // j mod RING: tile t's slot
+      constexpr int S1 = (T + 1) % C::RING, S2 = (T + 2) % C::RING, S3 = (T + 3) % C::RING;
+      constexpr int X = C::NM - C::P;         // MFMA behind which the barrier stands
+      int t3;
+      uint32_t bytes;
+      i32x4 rk, rv;
+      f32x16 sn, dn = start;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sn[e] = 0.f;
+      bf16x8 op[C::NM + C::P];
+      float x[16], p[16], ds[16];
+      u32x8 pd;
+#pragma unroll
+      for (int i = 0; i < C::P; ++i) op[i] = ahead[i];
+      auto logit = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        if constexpr (e < 16) {
+          x[e] = fmaf(s[e], a.scale_log2, nl);
+          asm volatile("" : "+v"(x[e]));  // holds the work here (it would otherwise sink to its uses)
         }
-#pragma unroll
-        for (int i = 0; i < C::DS; ++i) {
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_row<D>(kt_lds, off, kt, i), qf[i], s, 0, 0, 0);
-          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_row<D>(vt_lds, off, kt, i), dof[i], dp, 0, 0, 0);
+      };
+      auto prob = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        if constexpr (e < 16) {
+          p[e] = __builtin_amdgcn_exp2f(x[e]);
+          asm volatile("" : "+v"(p[e]));
         }
-        if (left < C::KB) {
-          const int vis = (int)left - 32 * kt - 4 * hh;
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (8 * (e / 4) + e % 4 >= vis) s[e] = -INFINITY;
+      };
+      // each stage works one element behind the stage before
+      auto element = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        logit(std::integral_constant<int, e + 2>{});
+        prob(std::integral_constant<int, e + 1>{});
+        ds[e] = p[e] * (C::START ? dp[e] : dp[e] + nd);
+        asm volatile("" : "+v"(ds[e]));
+        if constexpr (e % 2 == 1) pd[e / 2] = pack2_bf16(ds[e - 1], ds[e]);
+      };
+      logit(std::integral_constant<int, 0>{});
+      logit(std::integral_constant<int, 1>{});
+      prob(std::integral_constant<int, 0>{});
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<C::NM>([&](auto nc) {
+        constexpr int n = decltype(nc)::value;
+        // one wait for the operands of four MFMAs
+        if constexpr (n % 4 == 0) asm volatile("" ::"v"(op[n]), "v"(op[n + 1]), "v"(op[n + 2]), "v"(op[n + 3]));
+        if constexpr (n < C::NA) {
+          if constexpr (n % 2 == 0) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], qf[n / 2], sn, 0, 0, 0);
+          else dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], dof[n / 2], dn, 0, 0, 0);
+        } else {
+          constexpr int half = (n - C::NA) / C::DT, dt = (n - C::NA) % C::DT;
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], pack_half(pd, half), acc[dt], 0, 0, 0);
         }
-        u32x8 pk;
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, nl));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], a.scale_log2, nl));
-          pk[e / 2] = pack2_bf16(p0 * dp[e], p1 * dp[e + 1]);
+        // The scalar work of tile t + 3's loads is spread over the MFMAs before the
+        // barrier, the loads over those behind it: in one place they hold up the wave.
+        if constexpr (n == X - 6) t3 = fetch(j + 3);
+        if constexpr (n == X - 4) bytes = rows.bytes(t3);
+        if constexpr (n == X - 3) rk = load.rsrc(kbase, t3, bytes);
+        if constexpr (n == X - 2) rv = load.rsrc(vbase, t3, bytes);
+        if constexpr (n == X) {
+          publish();
+          load.issue(rk, ks[S3], wave);
         }
+        if constexpr (n == X + 1) load.issue(rv, vs[S3], wave);
+        constexpr int r = n + C::P;  // the operand to read now
+        if constexpr (r < C::NA) op[r] = read_a(r, S1);
+        else if constexpr (r < C::NM) op[r] = read_b(r - C::NA, T);
+        else op[r] = read_a(r - C::NM, S2);
+        // the elements whose turn it is
+        constexpr int e0 = (n * 16 + C::SPREAD - 1) / C::SPREAD;
+        static_for<2>([&](auto k) {
+          constexpr int e = e0 + decltype(k)::value;
+          if constexpr (e < 16 && e * C::SPREAD / 16 == n) element(std::integral_constant<int, e>{});
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int t = 0; t < C::DT; ++t)
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_col<D>(kt_lds, off, kt, half, t),
-                                                             pack_half(pk, half), acc[t], 0, 0, 0);
-      }
-      tile = next;
+      for (int i = 0; i < C::P; ++i) ahead[i] = op[C::NM + i];
+      s = sn;
+      dp = dn;
+      t0 = t1;
+      t1 = t2;
+      t2 = t3;
+      if ((uint32_t)t0 >= rows.whole) mask_tile(s, t0);
+    };
+    while (true) {
+      step(std::integral_constant<int, 0>{});
+      if (++j >= ntiles) break;
+      step(std::integral_constant<int, 1>{});
+      if (++j >= ntiles) break;
+      step(std::integral_constant<int, 2>{});
+      if (++j >= ntiles) break;
+      step(std::integral_constant<int, 3>{});
+      if (++j >= ntiles) break;
     }
+    wait_vmcnt<0>();  // loads past the end of the list still write LDS
   }
   if (!row_ok) return;
   if (a.dq_ranges > 1) {
@@ -356,16 +493,39 @@ void attn_bwd_dq_kernel(BwdArgs a) {
 
 // ---- dK and dV: one work-group per (head, query range, key group of 32 NW keys),
 // one wave per 32 keys.  Per 32-query sub-tile S = Q K^T and dP = dO V^T (lane: 16
-// queries of one key), then dV^T += dO^T P and dK^T += Q^T dS.  The sums and the
-// wave's K and V take 192 registers at D = 128, so one wave runs per SIMD there.
+// queries of one key), then dV^T += dO^T P and dK^T += Q^T dS.
+//
+// Step t holds S and dP of tile t + 1, then dV and dK of tile t: 32 MFMAs at D = 128,
+// 16 at 64.  The softmax of tile t is spread over the first two thirds of them, each
+// element behind one MFMA, and each MFMA's operand is read from LDS P MFMAs earlier.
+// S starts from -lse / s and dP from -delta, so an element takes a product, an
+// exponential, a product and its packing.  A tile lands in LDS a whole step before its
+// first read, and one barrier per step both publishes it and frees the slot of tile
+// t - 1.
+//
+// At D = 128 the sums, the wave's K and V and the operands in flight take some 350
+// registers, so one wave runs per SIMD.  It issues one instruction per 5 cycles at
+// most, so what a step costs is its count of instructions (the first form of this step,
+// with 340 of them, kept the matrix cores busy 48% of the time, LDS at a quarter of its
+// rate).
+template <int D>
+struct DkvCfg : BwdCfg<D, 32> {
+  using B = BwdCfg<D, 32>;
+  static constexpr int NA = 2 * B::DS, NB = 4 * B::DT, NM = NA + NB;  // MFMAs of a step
+  static constexpr int SPREAD = NM * 11 / 16;      // MFMAs that the softmax is spread over
+  static constexpr int P = 6;                      // MFMAs between an operand's read and its use
+  static constexpr int RING = 4;                   // tiles in LDS, Q and dO each
+  static constexpr int WAVES = D == 128 ? 1 : 2;   // per SIMD
+};
+
 template <int D, int NW, bool DENSE>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 128 ? 1 : 2, D == 128 ? 1 : 2)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DkvCfg<D>::WAVES, DkvCfg<D>::WAVES)))
 void attn_bwd_dkv_kernel(BwdArgs a) {
-  using C = BwdCfg<D>;
+  using C = DkvCfg<D>;
   constexpr int KEYS = 32 * NW, SUB = KEYS / C::KB;  // (sparse: a query block is SUB tiles)
-  __shared__ __attribute__((aligned(1024))) uint16_t qs[2][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t dos[2][C::TILE];
-  __shared__ __attribute__((aligned(1024))) float st[2][64 * C::KT];
+  __shared__ __attribute__((aligned(1024))) uint16_t qs[C::RING][C::TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t dos[C::RING][C::TILE];
+  __shared__ __attribute__((aligned(1024))) float st[C::RING][64];
   const int64_t n_g = (a.lk + KEYS - 1) / KEYS;
   const int64_t w = xcd_linear(blockIdx.x, gridDim.x);
   const int64_t pair = w / n_g;
@@ -430,67 +590,167 @@ void attn_bwd_dkv_kernel(BwdArgs a) {
   };
 
   const BwdOffsets<D> off(lane);
-  const TileLoad<D, NW> load(wave, lane);
+  const TileLoad<C, NW> load(wave, lane);
   const uint16_t* const qbase = a.q + bh * a.lq * D;
   const uint16_t* const dobase = a.d_o + bh * a.lq * D;
   const float* const stbase = a.stats + bh * a.n_q * a.block * 2;
+  const TileRows<C> rows(a.lq);
   auto issue = [&](int tile, int slot) {
-    load.issue(qbase, (int64_t)tile * C::KB, a.lq, qs[slot], wave);
-    load.issue(dobase, (int64_t)tile * C::KB, a.lq, dos[slot], wave);
-    if (wave < C::KT) dma_floats(stbase + ((int64_t)tile * C::KT + wave) * 64, st[slot] + 64 * wave, lane);
+    load.issue(load.rsrc(qbase, tile, rows.bytes(tile)), qs[slot], wave);
+    load.issue(load.rsrc(dobase, tile, rows.bytes(tile)), dos[slot], wave);
+    // (every wave loads the same statistics, so that all wait for as many loads)
+    dma_floats(raw_rsrc(stbase + (int64_t)tile * 64, tile < 0 ? 0u : 256u), st[slot], lane);
   };
+
   f32x16 dk[C::DT], dv[C::DT];
 #pragma unroll
   for (int t = 0; t < C::DT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[t][e] = dv[t][e] = 0.f;
 
-  int tile = next_tile();
-  if (tile >= 0) issue(tile, 0);
-  for (int j = 0; tile >= 0; ++j) {
-    const int next = next_tile();
+  int t0 = next_tile();
+  if (t0 >= 0) {
+    // MFMA n < NA of a step: S (n even) or dP of tile t + 1; n >= NA: dV or dK of tile t
+    auto read_a = [&](int n, int slot) -> bf16x8 {
+      return tile_row<D>(n % 2 == 0 ? qs[slot] : dos[slot], off, 0, n / 2);
+    };
+    auto read_b = [&](int m, int slot) -> bf16x8 {
+      return tile_col<D>(m % 2 == 0 ? dos[slot] : qs[slot], off, 0, m / (2 * C::DT), m / 2 % C::DT);
+    };
+    // where S and dP start from: element e is row 8 (e / 4) + 4 h + e % 4
+    auto read_init = [&](int g, int slot, f32x16& x, f32x16& y) {
+      const f32x4 l = *reinterpret_cast<const f32x4*>(st[slot] + 8 * g + 4 * hh);
+      const f32x4 d = *reinterpret_cast<const f32x4*>(st[slot] + 32 + 8 * g + 4 * hh);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[4 * g + e] = l[e];
+        y[4 * g + e] = d[e];
+      }
+    };
+    f32x16 s, dp;        // S and dP of tile t
+    f32x16 s1, dp1;      // the start of those of tile t + 1
+    bf16x8 ahead[C::P];  // operands of the next MFMAs
+
+    int t1 = next_tile(), t2 = next_tile();
+    issue(t0, 0);
+    issue(t1, 1);
+    issue(t2, 2);
     wait_vmcnt<0>();
     __syncthreads();
-    if (next >= 0) issue(next, (j + 1) & 1);
-    const uint16_t* qt = qs[j & 1];
-    const uint16_t* dt = dos[j & 1];
-    const float* stt = st[j & 1];
 #pragma unroll
-    for (int kt = 0; kt < C::KT; ++kt) {
-      f32x16 s, dp, nl;
+    for (int g = 0; g < 4; ++g) {
+      read_init(g, 0, s, dp);
+      read_init(g, 1, s1, dp1);
+    }
+    static_for<C::NA>([&](auto nc) {
+      constexpr int n = decltype(nc)::value;
+      const bf16x8 x = read_a(n, 0);
+      if constexpr (n % 2 == 0) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kf[n / 2], s, 0, 0, 0);
+      else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, vf[n / 2], dp, 0, 0, 0);
+    });
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 l = *reinterpret_cast<const float4*>(stt + 64 * kt + 8 * g + 4 * hh);
-        const float4 d = *reinterpret_cast<const float4*>(stt + 64 * kt + 32 + 8 * g + 4 * hh);
-        nl[4 * g] = l.x, nl[4 * g + 1] = l.y, nl[4 * g + 2] = l.z, nl[4 * g + 3] = l.w;
-        dp[4 * g] = d.x, dp[4 * g + 1] = d.y, dp[4 * g + 2] = d.z, dp[4 * g + 3] = d.w;
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < C::DS; ++i) {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_row<D>(qt, off, kt, i), kf[i], s, 0, 0, 0);
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_row<D>(dt, off, kt, i), vf[i], dp, 0, 0, 0);
-      }
+    for (int i = 0; i < C::P; ++i) ahead[i] = read_a(i, 1);
+
+    auto step = [&](auto tc) {
+      constexpr int T = decltype(tc)::value;  // t mod RING: tile t's slot
+      constexpr int S1 = (T + 1) % C::RING, S2 = (T + 2) % C::RING, S3 = (T + 3) % C::RING;
+      constexpr int X = C::NM - C::P;         // MFMA behind which the barrier stands
+      int t3;
+      uint32_t bytes;
+      i32x4 rq, rdo, rst;
+      f32x16 sn = s1, dn = dp1;
+      bf16x8 op[C::NM + C::P];
+      float x[16], p[16], ds[16];
       u32x8 pp, pd;
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, nl[e]));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[e + 1], a.scale_log2, nl[e + 1]));
-        pp[e / 2] = pack2_bf16(p0, p1);
-        pd[e / 2] = pack2_bf16(p0 * dp[e], p1 * dp[e + 1]);
-      }
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int t = 0; t < C::DT; ++t) {
-          dv[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_col<D>(dt, off, kt, half, t), pack_half(pp, half), dv[t],
-                                                          0, 0, 0);
-          dk[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile_col<D>(qt, off, kt, half, t), pack_half(pd, half), dk[t],
-                                                          0, 0, 0);
+      for (int i = 0; i < C::P; ++i) op[i] = ahead[i];
+      auto logit = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        if constexpr (e < 16) {
+          x[e] = s[e] * a.scale_log2;
+          asm volatile("" : "+v"(x[e]));  // holds the work here (it would otherwise sink to its uses)
         }
+      };
+      auto prob = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        if constexpr (e < 16) {
+          p[e] = __builtin_amdgcn_exp2f(x[e]);
+          asm volatile("" : "+v"(p[e]));
+        }
+      };
+      // each stage works one element behind the stage before
+      auto element = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        logit(std::integral_constant<int, e + 2>{});
+        prob(std::integral_constant<int, e + 1>{});
+        ds[e] = p[e] * dp[e];
+        asm volatile("" : "+v"(ds[e]));
+        if constexpr (e % 2 == 1) {
+          pp[e / 2] = pack2_bf16(p[e - 1], p[e]);
+          pd[e / 2] = pack2_bf16(ds[e - 1], ds[e]);
+        }
+      };
+      logit(std::integral_constant<int, 0>{});
+      logit(std::integral_constant<int, 1>{});
+      prob(std::integral_constant<int, 0>{});
+      __builtin_amdgcn_sched_barrier(0);
+      static_for<C::NM>([&](auto nc) {
+        constexpr int n = decltype(nc)::value;
+        // one wait for the operands of four MFMAs
+        if constexpr (n % 4 == 0) asm volatile("" ::"v"(op[n]), "v"(op[n + 1]), "v"(op[n + 2]), "v"(op[n + 3]));
+        if constexpr (n < C::NA) {
+          if constexpr (n % 2 == 0) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], kf[n / 2], sn, 0, 0, 0);
+          else dn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], vf[n / 2], dn, 0, 0, 0);
+        } else {
+          constexpr int m = n - C::NA, half = m / (2 * C::DT), dt = m / 2 % C::DT;
+          if constexpr (m % 2 == 0)
+            dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], pack_half(pp, half), dv[dt], 0, 0, 0);
+          else
+            dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[n], pack_half(pd, half), dk[dt], 0, 0, 0);
+        }
+        if constexpr (n == X - 6) t3 = next_tile();
+        if constexpr (n == X - 4) bytes = rows.bytes(t3);
+        if constexpr (n == X - 3) rq = load.rsrc(qbase, t3, bytes);
+        if constexpr (n == X - 2) rdo = load.rsrc(dobase, t3, bytes);
+        if constexpr (n == X - 1) rst = raw_rsrc(stbase + (int64_t)t3 * 64, t3 < 0 ? 0u : 256u);
+        if constexpr (n == X) {
+          publish();
+          load.issue(rq, qs[S3], wave);
+        }
+        if constexpr (n == X + 1) load.issue(rdo, dos[S3], wave);
+        if constexpr (n == X + 2) dma_floats(rst, st[S3], lane);
+        constexpr int r = n + C::P;  // the operand to read now
+        if constexpr (r < C::NA) op[r] = read_a(r, S1);
+        else if constexpr (r < C::NM) op[r] = read_b(r - C::NA, T);
+        else op[r] = read_a(r - C::NM, S2);
+        if constexpr (n >= C::NM - 4) read_init(n - (C::NM - 4), S2, s1, dp1);
+        // the elements whose turn it is
+        constexpr int e0 = (n * 16 + C::SPREAD - 1) / C::SPREAD;
+        static_for<2>([&](auto k) {
+          constexpr int e = e0 + decltype(k)::value;
+          if constexpr (e < 16 && e * C::SPREAD / 16 == n) element(std::integral_constant<int, e>{});
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+#pragma unroll
+      for (int i = 0; i < C::P; ++i) ahead[i] = op[C::NM + i];
+      s = sn;
+      dp = dn;
+      t0 = t1;
+      t1 = t2;
+      t2 = t3;
+    };
+    while (true) {
+      step(std::integral_constant<int, 0>{});
+      if (t0 < 0) break;
+      step(std::integral_constant<int, 1>{});
+      if (t0 < 0) break;
+      step(std::integral_constant<int, 2>{});
+      if (t0 < 0) break;
+      step(std::integral_constant<int, 3>{});
+      if (t0 < 0) break;
     }
-    tile = next;
+    wait_vmcnt<0>();  // loads past the end of the walk still write LDS
   }
   if (!key_ok) return;
   const int64_t at = (bh * a.lk + key) * D + 4 * hh, all = (int64_t)a.bh * a.lk * D;

@@ -44,6 +44,9 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
   }
   if (!(softmax_scale == softmax_scale) || isinf(softmax_scale))
     return report_error(SPARSTAR_ERR_INVALID_ARG, "softmax_scale must be finite");
+  // (lse / s has to stay finite)
+  if (softmax_scale > 0.f && softmax_scale < 1e-30f)
+    return report_error(SPARSTAR_ERR_INVALID_ARG, "softmax_scale must be at least 1e-30, or <= 0 for D^-1/2");
   const int64_t bh = int64_t(B) * H;
   const BwdPlan plan = attn_bwd_plan(bh, Lq, Lk, D, block_size, dense);
   if (!workspace && plan.total > 0) return report_error(SPARSTAR_ERR_WORKSPACE, "workspace is null");
@@ -73,6 +76,7 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
   a.stride = kv_stride;
   a.block = block_size;
   a.scale = float(sc);
+  a.inv_scale = float(1.0 / sc);
   a.scale_log2 = float(sc * 1.4426950408889634074);
   a.n_words = (a.n_q + 31) / 32;
   char* ws = static_cast<char*>(workspace);

@@ -153,8 +153,9 @@ struct BwdArgs {
   const int32_t* kv_indices;     // [BH, n_q, stride] (sparse only)
   int64_t lq, lk;
   int bh, n_q, n_k, stride, block;
-  float scale, scale_log2;       // softmax scale, and times log2(e)
-  float* stats;                  // [BH, n_q * block / 32, 2, 32]: -lse log2(e), -delta
+  float scale, inv_scale;        // softmax scale s, 1 / s
+  float scale_log2;              // s log2(e)
+  float* stats;                  // [BH, n_q * block / 32, 2, 32]: -lse / s, -delta
   uint32_t* bits;                // [BH, n_k, n_words]: which query blocks list each key block (sparse only)
   int n_words;                   // ceil(n_q / 32)
   float* part;                   // fp32 partial results of the ranges: dQ, then dK and dV in the same place
