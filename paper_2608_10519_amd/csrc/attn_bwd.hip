@@ -228,6 +228,11 @@ __device__ __forceinline__ void static_for(F&& f) {
   static_for(f, std::make_integer_sequence<int, N>{});
 }
 
+// Order of the work.  The dense passes give each XCD (and its L2) whole heads.  The sparse
+// ones go through a head on all XCDs at once, because the heads' lists differ in length:
+// with budgets from 0.5 to 1.5 of the mean, 24 heads, 11,520 queries, 84,032 keys, an XCD
+// per three heads took 14.0 ms, all XCDs per head 11.2 (equal budgets: 10.1 and 10.3).
+
 // ---- dQ: one work-group per (head, list range, query group of 32 NW rows), one
 // wave per 32 rows.  Per 32-key tile S^T = K Q^T and dP^T = V dO^T (lane: 16 keys of
 // one query), then dQ^T += K^T dS^T with dS rounded to bf16 once.  The step is that of
@@ -252,7 +257,7 @@ void attn_bwd_dq_kernel(BwdArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t ks[C::RING][C::TILE];
   __shared__ __attribute__((aligned(1024))) uint16_t vs[C::RING][C::TILE];
   const int64_t n_g = (a.lq + ROWS - 1) / ROWS;
-  const int64_t w = xcd_linear(blockIdx.x, gridDim.x);
+  const int64_t w = DENSE ? xcd_linear(blockIdx.x, gridDim.x) : blockIdx.x;
   const int64_t pair = w / n_g;
   const int qg = (int)(w - pair * n_g);
   const int64_t bh = pair / a.dq_ranges;
@@ -527,7 +532,8 @@ void attn_bwd_dkv_kernel(BwdArgs a) {
   __shared__ __attribute__((aligned(1024))) uint16_t dos[C::RING][C::TILE];
   __shared__ __attribute__((aligned(1024))) float st[C::RING][64];
   const int64_t n_g = (a.lk + KEYS - 1) / KEYS;
-  const int64_t w = xcd_linear(blockIdx.x, gridDim.x);
+  const int64_t items = (int64_t)a.bh * a.dkv_ranges * n_g;
+  const int64_t w = DENSE ? xcd_linear(blockIdx.x, gridDim.x) : blockIdx.x % items;
   const int64_t pair = w / n_g;
   const int kg = (int)(w - pair * n_g);
   const int64_t bh = pair / a.dkv_ranges;
@@ -535,6 +541,16 @@ void attn_bwd_dkv_kernel(BwdArgs a) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int l32 = lane % 32, hh = lane / 32;
 
+  // Key blocks that far more queries list than the average (forced ones: all of them) come
+  // first, in a turn of their own through the items: begun last they would run on alone.
+  if (!DENSE && a.long_first > 0) {
+    const uint32_t* words = a.bits + (bh * a.n_k + kg) * a.n_words;
+    int n = 0;
+    for (int i = lane; i < a.n_words; i += 64) n += __builtin_popcount(words[i]);
+#pragma unroll
+    for (int s = 32; s > 0; s /= 2) n += __shfl_xor(n, s);
+    if ((__builtin_amdgcn_readfirstlane(n) > a.long_first) != (blockIdx.x < items)) return;
+  }
   const int64_t key = (int64_t)kg * KEYS + wave * 32 + l32;
   const bool key_ok = key < a.lk;
   bf16x8 kf[C::DS], vf[C::DS];
@@ -802,7 +818,7 @@ static hipError_t launch_passes(const BwdArgs& a, hipStream_t stream) {
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.dq_ranges > 1) sum(a.part, nq, a.dq_ranges, nq, a.scale, a.dq);
   const int64_t dkv_grid = (int64_t)a.bh * a.dkv_ranges * ((a.lk + ROWS - 1) / ROWS);
-  attn_bwd_dkv_kernel<D, NW, DENSE><<<dkv_grid, 64 * NW, 0, stream>>>(a);
+  attn_bwd_dkv_kernel<D, NW, DENSE><<<dkv_grid * (!DENSE && a.long_first > 0 ? 2 : 1), 64 * NW, 0, stream>>>(a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.dkv_ranges > 1) {
     sum(a.part, 2 * nk, a.dkv_ranges, nk, a.scale, a.dk);

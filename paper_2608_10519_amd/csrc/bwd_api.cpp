@@ -85,6 +85,9 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
   a.part = reinterpret_cast<float*>(ws + plan.part);
   a.dq_ranges = plan.dq_ranges;
   a.dkv_ranges = plan.dkv_ranges;
+  // (twice the lists' entries per key block, if every row fills its stride)
+  if (!dense && plan.rounds)
+    a.long_first = int(std::max<int64_t>(1, 2 * int64_t(a.n_q) * std::min(kv_stride, a.n_k) / a.n_k));
   const hipError_t e = launch_attn_bwd(a, D, dense, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return report_error(SPARSTAR_ERR_HIP, hipGetErrorString(e));
   return clear_error();

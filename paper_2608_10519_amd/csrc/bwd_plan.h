@@ -11,6 +11,7 @@ namespace sparstar {
 
 struct BwdPlan {
   int dq_ranges, dkv_ranges;
+  bool rounds;  // the dK/dV pass has more work-groups than the chip holds
   size_t stats, bits, part, total;  // byte offsets of the workspace's regions, and its size
 };
 
@@ -30,9 +31,11 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   const int64_t nq = (lq + block - 1) / block, nk = (lk + block - 1) / block;
   BwdPlan p{};
   p.dq_ranges = bwd_ranges(bh * ((lq + rows - 1) / rows), 256 * 8 / waves, (lk + tile - 1) / tile);
-  p.dkv_ranges = bwd_ranges(bh * ((lk + rows - 1) / rows), 256 * (d == 128 ? 4 : 8) / waves, (lq + tile - 1) / tile);
+  const int64_t key_groups = bh * ((lk + rows - 1) / rows), held = 256 * (d == 128 ? 4 : 8) / waves;
+  p.dkv_ranges = bwd_ranges(key_groups, held, (lq + tile - 1) / tile);
   // (the sparse walk is cut at whole words of 32 query blocks)
   if (!dense) p.dkv_ranges = (int)std::min<int64_t>(p.dkv_ranges, std::max<int64_t>(1, (nq + 31) / 32));
+  p.rounds = key_groups * p.dkv_ranges > held;
   auto align = [](size_t x) { return (x + 255) & ~size_t(255); };
   p.stats = 0;
   p.bits = align(size_t(bh * nq * block) * 2 * sizeof(float));

@@ -160,6 +160,7 @@ struct BwdArgs {
   int n_words;                   // ceil(n_q / 32)
   float* part;                   // fp32 partial results of the ranges: dQ, then dK and dV in the same place
   int dq_ranges, dkv_ranges;     // ranges of each list's keys, and of the queries; 1: results go out at once
+  int long_first;                // key blocks on more lists than this go first (sparse only; 0: in order)
 };
 
 // The 8-bit key/value cache (cache.hip): e4m3 codes [BH, cap, D] and scale bytes
