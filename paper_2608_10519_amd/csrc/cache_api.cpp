@@ -88,17 +88,15 @@ extern "C" int sparstar_cache_read(const void* k_cache, const void* v_cache, con
 extern "C" size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size) {
   if (check_attn_sizes(B, H, Lq, Lk, D, block_size) != SPARSTAR_OK) return 0;
   const int64_t bh = int64_t(B) * H, nk = (Lk + block_size - 1) / block_size;
-  const int ranges = std::max(cache_attn_plan(bh, Lq, nk, block_size, false).ranges,
-                              cache_attn_plan(bh, Lq, nk, block_size, true).ranges);
+  // (a list's length is not known here)
+  const int ranges = Lq > 32 ? (nk >= kSplits ? kSplits : 1)
+                             : cache_attn_plan(bh, Lq, Lk, D, block_size, 0, true, true).ranges;
   return cache_attn_workspace(bh * Lq, D, ranges);
 }
 
 extern "C" void sparstar_internal_cache_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                              int64_t kv_stride, int64_t* out) {
-  const int64_t nk = (Lk + block_size - 1) / block_size;
-  const CachePlan p = cache_attn_plan(int64_t(B) * H, Lq, kv_stride == 0 ? nk : std::min(nk, kv_stride), block_size,
-                                      kv_stride == 0);
-  (void)D;
+  const CachePlan p = cache_attn_plan(int64_t(B) * H, Lq, Lk, D, block_size, kv_stride, kv_stride == 0, true);
   out[0] = p.waves;
   out[1] = p.ranges;
 }
@@ -124,9 +122,8 @@ static int cache_attn_common(const void* q, const void* k_cache, const void* v_c
   }
   if (!(softmax_scale == softmax_scale) || isinf(softmax_scale))
     return report_error(SPARSTAR_ERR_INVALID_ARG, "softmax_scale must be finite");
-  const int64_t nk = (Lk + block_size - 1) / block_size;
-  CachePlan plan = cache_attn_plan(bh, Lq, dense ? nk : std::min<int64_t>(nk, kv_stride), block_size, dense);
-  if (!workspace) plan.ranges = 1;
+  const CachePlan plan =
+      cache_attn_plan(bh, Lq, Lk, D, block_size, dense ? 0 : kv_stride, dense, workspace != nullptr);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
     return report_error(SPARSTAR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (workspace && workspace_bytes < cache_attn_workspace(bh * Lq, D, plan.ranges))
@@ -154,8 +151,11 @@ static int cache_attn_common(const void* q, const void* k_cache, const void* v_c
   a.stride = kv_stride;
   a.scale_log2 = float(sc * 1.4426950408889634074);
   a.ranges = plan.ranges;
+  a.rotation = plan.rotation;
+  a.spread_bits = plan.spread_bits;
+  a.grid = plan.grid;
   if (plan.ranges > 1) {
-    a.part_o = static_cast<float*>(workspace);
+    a.part_o = static_cast<uint16_t*>(workspace);
     a.part_meta = reinterpret_cast<float*>(static_cast<char*>(workspace) + cache_part_o_bytes(bh * Lq, D, plan.ranges));
   }
   const hipError_t e = launch_cache_attn(a, D, plan.waves, dense, static_cast<hipStream_t>(stream));

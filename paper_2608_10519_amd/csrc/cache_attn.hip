@@ -1,28 +1,28 @@
 // Attention over the 8-bit key/value cache (cache.hip), dense or over block lists.
 //
-// K and V stay 8-bit codes in memory, L2 and LDS: each tile moves half the bytes of a
-// bf16 one.  A lane turns the operands that it feeds to the matrix cores into bf16 in
-// registers, where code * 2^e is exact, so the only roundings are those of the bf16
-// forward: P to bf16 once, O to bf16 once.
+// K and V stay 8-bit codes in memory, L2 and on the way into LDS: a tile moves half the
+// bytes of a bf16 one.  The only roundings are those of the bf16 forward: P to bf16 once,
+// O to bf16 once.
 //
-// One work-group per (head, range of the list, 32 NW queries), one wave per 32
-// queries; S^T = K Q^T and O^T += V^T P^T as in attn_fwd.hip, whose MFMA layouts hold
-// here too.
+// Two kernels.  Calls of more than 32 query rows are bound by the matrix cores and the
+// VALU (cache_attn_kernel); up to 32 rows, single tokens above all, they stream the cache
+// (cache_token_kernel).
+#include <type_traits>
+#include <utility>
+
 #include "attn_device.h"
 
 namespace sparstar {
 
-template <int D, int NW>
+template <int D>
 struct CacheCfg {
   static constexpr int KB = attn_tile_keys(D);    // keys per tile
   static constexpr int KT = KB / 32;              // 32-key sub-tiles
-  static constexpr int DS = D / 16, DT = D / 32;  // MFMA k-steps over D, 32-row tiles of O^T
-  static constexpr int RB = D;                    // bytes per row
-  static constexpr int CPR = D / 16;              // 16-byte chunks per row
+  static constexpr int DS = D / 16, DT = D / 32;  // 16-column steps of a row, 32-row tiles of O^T
+  static constexpr int RB = D;                    // bytes per row of codes
+  static constexpr int CPR = D / 16;              // 16-byte chunks per row of codes
   static constexpr int RPD = 1024 / RB;           // rows per direct-to-LDS wave load
-  static constexpr int TILE = KB * RB;            // bytes per tile: 4 KB
-  static constexpr int N = 4 / NW;                // direct loads per wave and tile
-  static constexpr int RING = NW == 1 ? 4 : 3;    // tiles held in LDS, K and V each
+  static constexpr int TILE = KB * RB;            // bytes of codes per tile: 4 KB
   static_assert(TILE == 4096, "4 KB tiles");
 };
 
@@ -64,21 +64,69 @@ __device__ __forceinline__ void wait_loads_and_lds() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
-template <int D, int NW, bool DENSE>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void cache_attn_kernel(CacheAttnArgs a) {
-  using C = CacheCfg<D, NW>;
-  constexpr int ROWS = 32 * NW;
-  __shared__ __attribute__((aligned(1024))) uint8_t ks[C::RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint8_t vs[C::RING][C::TILE];
-  const int64_t n_g = (a.lq + ROWS - 1) / ROWS;
-  const int64_t w = xcd_linear(blockIdx.x, gridDim.x);
-  const int64_t pair = w / n_g;
-  const int qg = (int)(w - pair * n_g);
-  const int64_t bh = pair / a.ranges;
-  const int range = (int)(pair - bh * a.ranges);
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int l32 = lane % 32, hh = lane / 32;
+// Writes the lane's query row (its columns 32 t + 8 g + 4 h + 0..3): O and lse, or, with
+// several ranges, the range's unnormalised P V in fp16, scaled by a power of two so that
+// its largest magnitude lies in [0.5, 1), with the running max (log2 units), the two row
+// sums and the scale's exponent.  m, l and le are the row's; l == 0 means no key was seen
+// (a NaN passes on).
+template <int D>
+__device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, int64_t row, int range,
+                                           const f32x16 (&acc)[D / 32], float m, float l, float le, int hh) {
+  float amax = 0.f;
+  if (a.ranges > 1) {
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(acc[t][e]));
+    amax = half_swap_max(amax);
+  }
+  if (row >= a.lq) return;
+  const int64_t at = bh * a.lq + row;
+  if (a.ranges > 1) {
+    int ex = 0;
+    if (amax > 0.f && amax <= 3.402823466e38f) ex = __builtin_amdgcn_frexp_expf(amax);
+    ex = ex < -126 ? -126 : ex;
+    const float sc = __builtin_amdgcn_ldexpf(1.0f, -ex);
+    const int64_t prow = (int64_t)range * a.bh * a.lq + at;
+    _Float16* out = reinterpret_cast<_Float16*>(a.part_o) + prow * D + 4 * hh;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f16x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (_Float16)(acc[t][4 * g + e] * sc);
+        *reinterpret_cast<f16x4*>(out + 32 * t + 8 * g) = w;
+      }
+    if (hh == 0) reinterpret_cast<float4*>(a.part_meta)[prow] = make_float4(m, l, le, (float)ex);
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint16_t* out = a.o + at * D + 4 * hh;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<uint2*>(out + 32 * t + 8 * g) =
+          make_uint2(pack2_bf16(acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv),
+                     pack2_bf16(acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv));
+  if (a.lse != nullptr && hh == 0) a.lse[at] = le == 0.f ? -INFINITY : (m + log2f(le)) * 0.69314718055994530942f;
+}
+
+// ---- up to 32 query rows: one wave per (head, range of the list), with a ring of tiles of
+// its own and no barrier.  S^T = K Q^T and O^T += V^T P^T as in attn_fwd.hip, with the
+// operands turned into bf16 in registers; mostly empty products, but the matrix cores
+// could take 34 TB/s of codes this way.
+template <int D, bool DENSE>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void cache_token_kernel(CacheAttnArgs a) {
+  using C = CacheCfg<D>;
+  constexpr int RING = 4;
+  __shared__ __attribute__((aligned(1024))) uint8_t ks[RING][C::TILE];
+  __shared__ __attribute__((aligned(1024))) uint8_t vs[RING][C::TILE];
+  const int64_t bh = blockIdx.x / a.ranges;
+  const int range = (int)(blockIdx.x - bh * a.ranges);
+  const int lane = threadIdx.x, l32 = lane % 32, hh = lane / 32;
 
   // tokens that exist: rows past them are neither read nor attended to
   int64_t len = a.lk;
@@ -90,7 +138,7 @@ void cache_attn_kernel(CacheAttnArgs a) {
 
   // Q as the B operand of S^T = K Q^T.  A 16-byte read of a K row feeds two k-steps, so
   // step 2 i + j covers columns 32 i + 16 h + 8 j + (0..7).
-  const int64_t row = (int64_t)qg * ROWS + wave * 32 + l32;
+  const int64_t row = l32;
   const bool row_ok = row < a.lq;
   bf16x8 qf[C::DS];
 #pragma unroll
@@ -106,7 +154,7 @@ void cache_attn_kernel(CacheAttnArgs a) {
   {
     int n = n_blk;
     if constexpr (!DENSE) {
-      const int64_t r = bh * a.n_q + (int64_t)qg * ROWS / a.block;
+      const int64_t r = bh;  // (one query block)
       n = a.kv_num_blocks[r];
       n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
       list = a.kv_indices + r * a.stride;
@@ -142,10 +190,10 @@ void cache_attn_kernel(CacheAttnArgs a) {
     return Tile{b < 0 ? -1 : (b << sub_bits) + (j & ((1 << sub_bits) - 1)), s};
   };
 
-  uint32_t loff[C::N];
+  uint32_t loff[4];
 #pragma unroll
-  for (int i = 0; i < C::N; ++i) {
-    const int r = C::RPD * (C::N * wave + i) + lane / C::CPR;
+  for (int i = 0; i < 4; ++i) {
+    const int r = C::RPD * i + lane / C::CPR;
     loff[i] = (uint32_t)(r * C::RB + 16 * ((lane % C::CPR) ^ cache_swz<D>(r)) - 1024 * i);
   }
   const uint8_t* const kbase = a.k_cache + bh * a.cap * D;
@@ -154,9 +202,9 @@ void cache_attn_kernel(CacheAttnArgs a) {
     int64_t left = tile < 0 ? 0 : len - (int64_t)tile * C::KB;
     left = left < 0 ? 0 : (left > C::KB ? C::KB : left);
     const int64_t at = tile < 0 ? 0 : (int64_t)tile * C::TILE;
-    const uint32_t bytes = (uint32_t)left * C::RB, m0 = (uint32_t)(C::N * wave) * 1024u;
-    dma_tile<C::N>(lds_addr(ks[slot]) + m0, loff, raw_rsrc(kbase + at, bytes));
-    dma_tile<C::N>(lds_addr(vs[slot]) + m0, loff, raw_rsrc(vbase + at, bytes));
+    const uint32_t bytes = (uint32_t)left * C::RB;
+    dma_tile<4>(__builtin_amdgcn_readfirstlane(lds_addr(ks[slot])), loff, raw_rsrc(kbase + at, bytes));
+    dma_tile<4>(__builtin_amdgcn_readfirstlane(lds_addr(vs[slot])), loff, raw_rsrc(vbase + at, bytes));
   };
 
   // per-lane LDS offsets: K row l32, chunk 2 i + h; V rows of the transpose read
@@ -180,24 +228,24 @@ void cache_attn_kernel(CacheAttnArgs a) {
   if (ntiles > 0) {
     load_batch(0);
     Tile cur = fetch(0);
-    Tile ahead[C::RING - 1];
+    Tile ahead[RING - 1];
     ahead[0] = cur;
     issue(cur.t, 0);
 #pragma unroll
-    for (int i = 1; i < C::RING - 1; ++i) {
+    for (int i = 1; i < RING - 1; ++i) {
       ahead[i] = fetch(i);
       issue(ahead[i].t, i);
     }
     int slot = 0;
     for (int j = 0; j < ntiles; ++j) {
-      const Tile nt = fetch(j + C::RING - 1);
-      wait_loads_and_lds<2 * C::N*(C::RING - 2)>();  // tile j, with the tiles issued after it outstanding
+      const Tile nt = fetch(j + RING - 1);
+      wait_loads_and_lds<2 * 4 * (RING - 2)>();  // tile j, with the tiles issued after it outstanding
       __syncthreads();
-      issue(nt.t, slot == 0 ? C::RING - 1 : slot - 1);
+      issue(nt.t, slot == 0 ? RING - 1 : slot - 1);
       cur = ahead[0];
 #pragma unroll
-      for (int i = 0; i + 1 < C::RING - 1; ++i) ahead[i] = ahead[i + 1];
-      ahead[C::RING - 2] = nt;
+      for (int i = 0; i + 1 < RING - 1; ++i) ahead[i] = ahead[i + 1];
+      ahead[RING - 2] = nt;
       const uint8_t* kt_lds = ks[slot];
       const uint8_t* vt_lds = vs[slot];
       const float ksc = __uint_as_float((uint32_t)(cur.s & 255) << 23);
@@ -258,42 +306,455 @@ void cache_attn_kernel(CacheAttnArgs a) {
             acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(u, vsc), pack_half(pk, half), acc[t], 0, 0, 0);
           }
       }
-      slot = slot + 1 == C::RING ? 0 : slot + 1;
+      slot = slot + 1 == RING ? 0 : slot + 1;
     }
     wait_vmcnt<0>();  // loads past the end of the list still write LDS
   }
 
-  l_run = half_swap_sum(l_run);
-  le_run = half_swap_sum(le_run);
-  if (!row_ok) return;
-  const int64_t at = bh * a.lq + row;
-  if (a.ranges > 1) {
-    const int64_t prow = (int64_t)range * a.bh * a.lq + at;
-    float* out = a.part_o + prow * D + 4 * hh;
+  store_rows<D>(a, bh, row, range, acc, m_run, half_swap_sum(l_run), half_swap_sum(le_run), hh);
+}
+
+// ---- more than 32 query rows: one work-group per (head, range of the list, 32 NW rows),
+// one wave per 32 rows, two waves per SIMD.
+//
+// What bounds it is the VALU: a 32x32x16 MFMA takes the time of 7.7 VALU instructions
+// (two waves per SIMD), the softmax takes 4.2 of those per MFMA at D = 128, and turning
+// every K and V operand into bf16 takes 4 more in each wave.  So V is turned into bf16
+// once per work-group: each wave takes its share of a tile from LDS and puts it back in
+// the layout of the transpose read (0.5 conversions per MFMA and wave with four waves, 1
+// with two); K is converted as it is read (2 per MFMA).  Products of codes would need no
+// conversion of K, with Q as the sum of two e4m3 numbers: but v_mfma_f32_32x32x64_f8f6f4
+// aligns the products of eight columns to the largest of them with 13 bits, which was
+// measured to cost up to 8e-4 of the lse.
+//
+// Step t: S of tile t + 1 and P V of tile t - 1 on the matrix cores, the softmax of tile t
+// spread evenly under them, V of tile t converted.  One barrier per step, behind which the
+// converted tile and the next raw tiles can be read, and the raw ones that were read are
+// overwritten; loads have two steps to land.
+// The softmax keeps a running max that is only refreshed when some lane's sum of a tile's
+// P exceeds 2^8 (attn_fwd.hip); the row sum of the bf16 P comes from 4x4x4 MFMAs.
+template <int D, int NW>
+struct CachePipe : CacheCfg<D> {
+  using B = CacheCfg<D>;
+  static constexpr int N = 4 / NW;              // direct loads per wave and raw tile
+  static constexpr int RING = 3;                // raw tiles in LDS, K and V each
+  static constexpr int NA = B::KT * B::DS;      // MFMAs of S
+  static constexpr int NB = 2 * B::KT * B::DT;  // MFMAs of P V
+  static constexpr int NE = 16 * B::KT;         // elements of S per lane
+  static constexpr int EPU = NE / 16;           // elements per MFMA
+  static constexpr int VTILE = B::KB * D;       // elements of a converted tile
+  static constexpr int CV = 4 / NW;             // 16-code pieces of V that a lane converts
+  static_assert(NA == 8 && NB == 8, "a step is 16 MFMAs");
+};
+
+// f(0), .., f(N - 1) with each index a compile-time constant
+template <class F, int... I>
+__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for(f, std::make_integer_sequence<int, N>{});
+}
+
+template <int D, int NW, bool DENSE>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void cache_attn_kernel(CacheAttnArgs a) {
+  using C = CachePipe<D, NW>;
+  constexpr int ROWS = 32 * NW;
+  __shared__ __attribute__((aligned(1024))) uint8_t kr[C::RING][C::TILE];
+  __shared__ __attribute__((aligned(1024))) uint8_t vr[C::RING][C::TILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t vb[2][C::VTILE];
+
+  // Work item: as in attn_fwd.hip, the query groups of a (head, range) pair are dealt out
+  // to 2^spread_bits XCDs, each of which runs its share of a pair after the other.
+  const uint32_t n_g = (uint32_t)((a.lq + ROWS - 1) / ROWS);
+  uint32_t gi, pair;
+  int qg;
+  if (a.spread_bits == 3) {
+    pair = blockIdx.x / n_g;
+    qg = (int)(blockIdx.x - pair * n_g);
+    gi = (uint32_t)qg >> 3;
+  } else {
+    const uint32_t n_u = (n_g + (1u << a.spread_bits) - 1) >> a.spread_bits;
+    const uint32_t id = blockIdx.x / 8, ui = id / n_u;
+    gi = id - ui * n_u;
+    const uint32_t unit = ui * 8 + (blockIdx.x + ui) % 8;
+    pair = unit >> a.spread_bits;
+    qg = (int)((gi << a.spread_bits) + (unit & ((1u << a.spread_bits) - 1)));
+  }
+  if (pair >= (uint32_t)(a.bh * a.ranges) || qg >= (int)n_g) return;  // uniform: past the last unit or group
+  const int64_t bh = pair / (uint32_t)a.ranges;
+  const int range = (int)(pair - (uint32_t)bh * (uint32_t)a.ranges);
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int l32 = lane % 32, hh = lane / 32;
+
+  // tokens that exist: rows past them are neither read nor attended to
+  int64_t len = a.lk;
+  if (a.lens != nullptr) {
+    const int n = a.lens[bh / a.heads];
+    len = n < 0 ? 0 : (n < a.lk ? n : a.lk);
+  }
+  const int n_blk = (int)((len + a.block - 1) / a.block);
+
+  // ---- Q as the B operand of S^T = K Q^T.  A 16-byte read of a K row feeds two k-steps, so
+  // step 2 i + j covers columns 32 i + 16 h + 8 j + (0..7).
+  const int64_t row = (int64_t)qg * ROWS + wave * 32 + l32;
+  const bool row_ok = row < a.lq;
+  bf16x8 qf[C::DS];
+#pragma unroll
+  for (int s = 0; s < C::DS; ++s) {
+    const uint16_t* p = a.q + (bh * a.lq + (row_ok ? row : 0)) * D + 32 * (s / 2) + 16 * hh + 8 * (s % 2);
+    const uint4 u = row_ok ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+    qf[s] = __builtin_bit_cast(bf16x8, u);
+  }
+
+  // ---- the range's key blocks: an even share of the list's entries, or of all blocks,
+  // walked from `rot` on and around (see attn_fwd.hip for why)
+  int first = 0, cnt, rot = 0;
+  const int32_t* list = nullptr;
+  {
+    int n = n_blk;
+    if constexpr (!DENSE) {
+      const int64_t r = bh * a.n_q + qg;
+      n = a.kv_num_blocks[r];
+      n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
+      list = a.kv_indices + r * a.stride;
+    }
+    first = __builtin_amdgcn_readfirstlane((int)((int64_t)n * range / a.ranges));
+    cnt = __builtin_amdgcn_readfirstlane((int)((int64_t)n * (range + 1) / a.ranges)) - first;
+    if (!DENSE && a.rotation > 0 && n < n_blk)
+      rot = (int)((int64_t)(gi % (uint32_t)a.rotation) * cnt / a.rotation);
+  }
+  // Entries 64 at a time in VGPRs: the block and its scale bytes.  One that names no
+  // block gives -1, whose tiles are loaded as zeros and masked.
+  constexpr int SUB = (DENSE ? 64 : ROWS) / C::KB;  // tiles per entry (dense: of 64 keys)
+  const int64_t scale_at = bh * ((a.cap + a.block - 1) / a.block);
+  int breg = -1, sreg = 0, lbase = 0;
+  // (dense entries are 64 keys whatever the block size)
+  const int e_bits = DENSE ? (a.block == 128 ? 1 : 0) : 0;
+  if constexpr (DENSE) {
+    first <<= e_bits;
+    cnt <<= e_bits;
+  }
+  auto load_batch = [&](int base) {
+    lbase = base;
+    int b = -1;
+    if (base + lane < cnt) {
+      const int e = base + lane + rot;
+      b = DENSE ? first + base + lane : list[first + (e >= cnt ? e - cnt : e)];
+    }
+    const int blk = b >> e_bits;
+    if (b < 0 || blk >= n_blk) b = -1;
+    breg = b;
+    sreg = 127 | 127 << 8;
+    if (b >= 0) sreg = (int)a.k_scale[scale_at + blk] | (int)a.v_scale[scale_at + blk] << 8;
+    asm volatile("; list batch %0 %1" ::"v"(breg), "v"(sreg));
+  };
+  const int ntiles = cnt * SUB;
+  struct Tile {
+    int t;  // KB-key tile of the cache, -1: none
+    int s;  // scale bytes
+  };
+  auto fetch = [&](int j) -> Tile {
+    if (j >= ntiles) return Tile{-1, 127 | 127 << 8};
+    const int e = j / SUB;
+    if (e >= lbase + 64) load_batch(lbase + 64);
+    const int b = __builtin_amdgcn_readlane(breg, e - lbase);
+    return Tile{b < 0 ? -1 : b * SUB + j % SUB, __builtin_amdgcn_readlane(sreg, e - lbase)};
+  };
+
+  // ---- raw tiles: K rows with their chunks permuted (read by rows), V as it is
+  // (the instruction adds 1024 i to the i-th load of a wave)
+  const uint32_t voffs[2] = {(uint32_t)(1024 * C::N * wave + 16 * lane), (uint32_t)(1024 * C::N * wave + 16 * lane)};
+  uint32_t koffs[C::N];
+#pragma unroll
+  for (int i = 0; i < C::N; ++i) {
+    const int r = C::RPD * (C::N * wave + i) + lane / C::CPR;
+    koffs[i] = (uint32_t)(r * C::RB + 16 * ((lane % C::CPR) ^ cache_swz<D>(r)) - 1024 * i);
+  }
+  const uint32_t kr0 = lds_addr(kr), vr0 = lds_addr(vr);
+  const uint8_t* const kbase = a.k_cache + bh * a.cap * D;
+  const uint8_t* const vbase = a.v_cache + bh * a.cap * D;
+  const uint32_t n_whole = (uint32_t)(len / C::KB), last_bytes = (uint32_t)(len % C::KB) * C::RB;
+  auto issue = [&](const uint8_t* base, int tile, uint32_t slot, const uint32_t* offs) {
+    const uint32_t bytes = (uint32_t)tile < n_whole ? C::TILE : ((uint32_t)tile == n_whole ? last_bytes : 0u);
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane(slot + (uint32_t)(C::N * wave) * 1024u);
+    dma_tile<C::N>(m0, offs, raw_rsrc(base + (int64_t)tile * C::TILE, bytes));
+  };
+
+  // ---- per-lane LDS offsets
+  uint32_t koff[C::DS / 2];  // K row l32, chunk 2 i + h
+#pragma unroll
+  for (int i = 0; i < C::DS / 2; ++i) koff[i] = (uint32_t)(l32 * C::RB + 16 * ((2 * i + hh) ^ cache_swz<D>(l32)));
+  // converted V: rows of 2 D bytes, 16-byte chunk c of row r at c ^ vswz(r), as attn_fwd.hip has it
+  constexpr int VRB = 2 * D, VRPB = 256 / VRB, VCPR = D / 8;
+  auto vswz = [](int r) { return (((r / VRPB) & 3) << 2) & (VCPR - 1); };
+  uint32_t voff[C::DT];  // transpose read: rows 4 h + (0..3), columns 32 t + l % 32
+  {
+    const int sl = lane & 15, r = 4 * hh + (sl >> 2);
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(out + 32 * t + 8 * g) =
-            make_float4(acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]);
-    if (hh == 0) reinterpret_cast<float4*>(a.part_meta)[prow] = make_float4(m_run, l_run, le_run, 0.f);
-    return;
+      voff[t] = (uint32_t)(r * VRB + 16 * ((4 * t + 2 * (lane >> 4 & 1) + ((sl & 3) >> 1)) ^ vswz(r)) + 8 * (sl & 1));
   }
-  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;  // (a NaN passes on)
-  uint16_t* out = a.o + at * D + 4 * hh;
+  // what the lane converts: 16 codes from byte cv_src + 1024 i of the tile; they go to two
+  // neighbouring chunks (8 or 16 rows further per i, where the permutation is the same)
+  const uint32_t cv_src = (uint32_t)(16 * lane + 1024 * C::CV * wave);
+  uint32_t cv_dst;
+  {
+    const int r = (int)cv_src / C::RB, c = (int)cv_src % C::RB / 16;
+    cv_dst = (uint32_t)(r * VRB + 16 * ((2 * c) ^ vswz(r)));
+  }
+
+  const s16x4 one4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};  // bf16 1.0
+  auto mask_tile = [&](f32x16* x, int tile) {
+    const int64_t left = tile < 0 ? 0 : len - (int64_t)tile * C::KB;
+    const int vis = (int)(left < 0 ? 0 : (left > C::KB ? C::KB : left)) - 4 * hh;
+    asm volatile("; mask");  // (keeps the branch around this: it is rarely taken)
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (kt * 32 + 8 * (e / 4) + (e % 4) >= vis) x[kt][e] = -INFINITY;
+  };
+  auto tile_max = [&](const f32x16* x) -> float {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[kt][e]);
+    return mx;
+  };
+  const float sl2 = a.scale_log2;
+
+  f32x16 acc[C::DT];
 #pragma unroll
   for (int t = 0; t < C::DT; ++t)
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<uint2*>(out + 32 * t + 8 * g) =
-          make_uint2(pack2_bf16(acc[t][4 * g] * inv, acc[t][4 * g + 1] * inv),
-                     pack2_bf16(acc[t][4 * g + 2] * inv, acc[t][4 * g + 3] * inv));
-  if (a.lse != nullptr && hh == 0)
-    a.lse[at] = le_run == 0.f ? -INFINITY : (m_run + log2f(le_run)) * 0.69314718055994530942f;
+    for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f, le_run = 0.f;  // max in the log2 domain; sums of the lane's half of the keys
+
+  if (ntiles > 0) {
+    // K operands: 16-byte piece o of a tile's rows holds those of MFMAs 2 o and 2 o + 1 of S
+    constexpr int NK = C::NA / 2, KPT = NK / C::KT;
+    auto read_k = [&](int o, uint32_t slot) -> uint4 {
+      return *reinterpret_cast<const uint4*>(&kr[0][0] + slot + o / KPT * 32 * C::RB + koff[o % KPT]);
+    };
+    auto k_operand = [&](uint4 u, int j, float sc) { return decode8(j == 0 ? make_uint2(u.x, u.y) : make_uint2(u.z, u.w), sc); };
+    auto k_scale = [](int s) { return __uint_as_float((uint32_t)(s & 255) << 23); };
+    // V^T operand of P V: step m = (2 kt + half) DT + dt
+    auto read_v = [&](int m, int buf) -> bf16x8 {
+      typedef __attribute__((address_space(3))) uint16_t lds16;
+      const lds16* p = (const lds16*)vb[0] + (voff[m % C::DT] / 2 + 16 * (m / C::DT) * D + buf * C::VTILE);
+      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+      const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 8 * D));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto convert = [&](uint4 u, float sc, int i, uint16_t* tile) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t x = k == 0 ? u.x : u.z, y = k == 0 ? u.y : u.w;
+        uint4 r;
+        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, sc, false));
+        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, sc, true));
+        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, sc, false));
+        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, sc, true));
+        *reinterpret_cast<uint4*>(reinterpret_cast<char*>(tile) + 2048 * i + (cv_dst ^ (uint32_t)(16 * k))) = r;
+      }
+    };
+    // ---- prologue: raw K of tiles 0..2, V of 0..1; S of tile 0
+    load_batch(0);
+    Tile t0 = fetch(0), t1 = fetch(1), t2 = fetch(2), t3 = fetch(3);
+    issue(kbase, t0.t, kr0 + 0 * C::TILE, koffs);
+    issue(kbase, t1.t, kr0 + 1 * C::TILE, koffs);
+    issue(vbase, t0.t, vr0 + 0 * C::TILE, voffs);
+    issue(kbase, t2.t, kr0 + 2 * C::TILE, koffs);
+    issue(vbase, t1.t, vr0 + 1 * C::TILE, voffs);
+    issue(vbase, t2.t, vr0 + 2 * C::TILE, voffs);
+    // "P V of tile -1" multiplies zeros
+    for (int i = threadIdx.x; i < C::VTILE / 8; i += 64 * NW) reinterpret_cast<uint4*>(vb[1])[i] = make_uint4(0, 0, 0, 0);
+    wait_vmcnt<0>();
+    __syncthreads();
+    f32x16 s[C::KT];  // S^T of tile t
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kt][e] = 0.f;
+    static_for<C::NA>([&](auto nc) {
+      constexpr int n = decltype(nc)::value, kt = n / C::DS;
+      s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(read_k(n / 2, 0u), n % 2, k_scale(t0.s)), qf[n % C::DS],
+                                                      s[kt], 0, 0, 0);
+    });
+    if ((uint32_t)t0.t >= n_whole) mask_tile(s, t0.t);
+    m_run = half_swap_max(tile_max(s)) * sl2;  // O and the sums are still zero
+    u32x8 pp[C::KT];  // bf16 pairs of P^T of tile t - 1
+#pragma unroll
+    for (int kt = 0; kt < C::KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pp[kt][i] = 0u;
+    __syncthreads();  // slot 0 of K is free
+    issue(kbase, t3.t, kr0, koffs);
+
+    // Raw tile j lies in slot j % RING.  At the barrier of step t the loads of K(t + 2) and
+    // V(t + 1) have landed; V(t + 3) and K(t + 4) follow into the slots of V(t) and K(t + 1).
+    int j = 0;
+    uint32_t slot0 = 0, slot1 = C::TILE;  // of raw tiles t and t + 1, in bytes
+    auto step = [&](auto tc) {
+      constexpr int T = decltype(tc)::value;  // t mod 2
+      constexpr int vt = (T + 1) % 2;               // buffer of V(t - 1)
+      uint16_t* const vt_next = vb[T % 2];          // V(t)
+      f32x16 sn[C::KT];
+      u32x8 pk[C::KT];
+      uint4 kop[NK];
+      bf16x8 vop[C::NB];
+      uint4 raw[C::CV];
+#pragma unroll
+      for (int n = 0; n < NK; ++n) kop[n] = read_k(n, slot1);
+      float x[C::NE], p[C::NE], se = 0.f;
+      f32x4 st4 = {0.f, 0.f, 0.f, 0.f};
+      const float neg_m = m_run == -INFINITY ? INFINITY : -m_run;  // (no key seen yet: takes the exact path)
+      const float vsc = __uint_as_float((uint32_t)(t0.s >> 8) << 23), ksc = k_scale(t1.s);
+      auto row_sum = [&](auto ic) {  // adds pairs i - 1 and i of P
+        constexpr int i = decltype(ic)::value;
+        const uint2 u = make_uint2(pk[i / 8][i % 8 - 1], pk[i / 8][i % 8]);
+        st4 = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(one4, __builtin_bit_cast(s16x4, u), st4, 0, 0, 0);
+      };
+      auto logit = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        if constexpr (e < C::NE) {
+          x[e] = fmaf(s[e / 16][e % 16], sl2, neg_m);
+          asm volatile("" : "+v"(x[e]));  // holds the work here (it would otherwise sink to its uses)
+        }
+      };
+      auto prob = [&](auto ec) {
+        constexpr int e = decltype(ec)::value;
+        if constexpr (e < C::NE) {
+          p[e] = __builtin_amdgcn_exp2f(x[e]);
+          asm volatile("" : "+v"(p[e]));
+        }
+      };
+      auto element = [&](auto ec) {  // each stage works one element behind the stage before
+        constexpr int e = decltype(ec)::value;
+        logit(std::integral_constant<int, e + 2>{});
+        prob(std::integral_constant<int, e + 1>{});
+        se = e == 0 ? p[0] : se + p[e];
+        asm volatile("" : "+v"(se));
+        if constexpr (e % 2 == 1) {
+          pk[e / 16][e % 16 / 2] = pack2_bf16(p[e - 1], p[e]);
+        }
+      };
+      auto unit = [&](auto uc) {  // the softmax under one MFMA
+        static_for<C::EPU>([&](auto k) {
+          element(std::integral_constant<int, decltype(uc)::value * C::EPU + decltype(k)::value>{});
+        });
+      };
+      logit(std::integral_constant<int, 0>{});
+      logit(std::integral_constant<int, 1>{});
+      prob(std::integral_constant<int, 0>{});
+      __builtin_amdgcn_sched_barrier(0);
+      // ---- S of tile t + 1; each operand is converted one MFMA ahead
+      bf16x8 kb = k_operand(kop[0], 0, ksc);
+      static_for<C::NA>([&](auto nc) {
+        constexpr int n = decltype(nc)::value, kt = n / C::DS;
+        if constexpr (n % C::DS == 0)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sn[kt][e] = 0.f;
+        sn[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb, qf[n % C::DS], sn[kt], 0, 0, 0);
+        if constexpr (n + 1 < C::NA) kb = k_operand(kop[(n + 1) / 2], (n + 1) % 2, ksc);
+        if constexpr (n >= 4) vop[n - 4] = read_v(n - 4, vt);
+        if constexpr (n == C::NA - 1)
+#pragma unroll
+          for (int k = 0; k < C::CV; ++k) raw[k] = *reinterpret_cast<const uint4*>(&vr[0][0] + slot0 + cv_src + 1024 * k);
+        unit(std::integral_constant<int, n>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      // ---- P V of tile t - 1, while V(t) is converted
+      static_for<C::NB>([&](auto mc) {
+        constexpr int m = decltype(mc)::value, kt = m / C::DT / 2, half = m / C::DT % 2, dt = m % C::DT;
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[m], pack_half(pp[kt], half), acc[dt], 0, 0, 0);
+        if constexpr (m + 4 < C::NB) vop[m + 4] = read_v(m + 4, vt);
+        if constexpr (m < C::CV) convert(raw[m], vsc, m, vt_next);
+        unit(std::integral_constant<int, 8 + m>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      static_for<C::NE / 4>([&](auto k) { row_sum(std::integral_constant<int, 2 * decltype(k)::value + 1>{}); });
+      float st = st4[0];
+      const Tile t4 = fetch(j + 4);
+      wait_loads_and_lds<2 * C::N>();  // (all but the youngest two, V(t + 2) and K(t + 3))
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      issue(vbase, t3.t, vr0 + slot0, voffs);
+      issue(kbase, t4.t, kr0 + slot1, koffs);
+
+      // A lane's sum of its P stays <= 2^8 whenever every p does; otherwise the exact path:
+      // the tile's max, a rescale of O (tiles up to t - 1) and both sums, and P again.
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(st <= 256.f)) != 0, 0)) {
+        const float mx = half_swap_max(tile_max(s)) * sl2;
+        if (mx > m_run) {
+          float alpha = 0.f;
+          const float dm = mx - m_run;
+          if (dm > 128.f) {
+            m_run = mx;
+          } else {
+            const float k = ceilf(dm);
+            alpha = __builtin_amdgcn_ldexpf(1.f, -(int)k);
+            m_run += k;
+          }
+          l_run *= alpha;
+          le_run *= alpha;
+#pragma unroll
+          for (int d = 0; d < C::DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+        }
+        st = 0.f;
+        se = 0.f;
+        const float off = m_run == -INFINITY ? 0.f : -m_run;
+#pragma unroll
+        for (int e = 0; e < C::NE; e += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], sl2, off));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16 + 1], sl2, off));
+          se += p0;
+          se += p1;
+          const uint32_t u = pack2_bf16(p0, p1);
+          st += bf16_lo(u) + bf16_hi(u);
+          pk[e / 16][e % 16 / 2] = u;
+        }
+      }
+      l_run += st;
+      le_run += se;
+      if (__builtin_expect((uint32_t)t1.t >= n_whole, 0)) mask_tile(sn, t1.t);
+#pragma unroll
+      for (int kt = 0; kt < C::KT; ++kt) {
+        s[kt] = sn[kt];
+        pp[kt] = pk[kt];
+      }
+      t0 = t1;
+      t1 = t2;
+      t2 = t3;
+      t3 = t4;
+      slot0 = slot1;
+      slot1 = slot1 == 2 * C::TILE ? 0 : slot1 + C::TILE;
+    };
+    while (true) {
+      step(std::integral_constant<int, 0>{});
+      if (++j >= ntiles) break;
+      step(std::integral_constant<int, 1>{});
+      if (++j >= ntiles) break;
+    }
+    // P V of the last tile, which the last step converted
+#pragma unroll
+    for (int m = 0; m < C::NB; ++m)
+      acc[m % C::DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          read_v(m, (ntiles - 1) % 2), pack_half(pp[m / C::DT / 2], m / C::DT % 2), acc[m % C::DT], 0, 0, 0);
+    wait_vmcnt<0>();  // loads past the end of the list still write LDS
+  }
+  store_rows<D>(a, bh, row, range, acc, m_run, half_swap_sum(l_run), half_swap_sum(le_run), hh);
 }
 
 // Joins the ranges of one row: with M = max_r m_r and w_r = 2^(m_r - M),
-// O = sum w_r A_r / sum w_r l_r and lse = ln 2 (M + log2 sum w_r le_r).  D / 8 threads
+// O = sum w_r 2^e_r A_r / sum w_r l_r and lse = ln 2 (M + log2 sum w_r le_r).  D / 8 threads
 // per row and G groups of them, each over every G-th range.
 template <int D, int G>
 __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a) {
@@ -320,14 +781,11 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a) {
     for (int r = g; r < a.ranges; r += G) {
       const int64_t p = (int64_t)r * rows + row;
       const float4 x = meta[p];
-      const float4 u = *reinterpret_cast<const float4*>(a.part_o + p * D + 8 * c);
-      const float4 v = *reinterpret_cast<const float4*>(a.part_o + p * D + 8 * c + 4);
+      const f16x8 u = *reinterpret_cast<const f16x8*>(reinterpret_cast<const _Float16*>(a.part_o) + p * D + 8 * c);
       if (x.y == 0.f) continue;  // no key seen; NaN passes on
-      const float t = __builtin_amdgcn_exp2f(x.x - m);
-      acc[0] = fmaf(t, u.x, acc[0]), acc[1] = fmaf(t, u.y, acc[1]);
-      acc[2] = fmaf(t, u.z, acc[2]), acc[3] = fmaf(t, u.w, acc[3]);
-      acc[4] = fmaf(t, v.x, acc[4]), acc[5] = fmaf(t, v.y, acc[5]);
-      acc[6] = fmaf(t, v.z, acc[6]), acc[7] = fmaf(t, v.w, acc[7]);
+      const float t = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(x.x - m), (int)x.w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(t, (float)u[e], acc[e]);
     }
   if constexpr (G > 1) {
 #pragma unroll
@@ -347,31 +805,30 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a) {
   if (a.lse != nullptr && c == 0) a.lse[row] = le == 0.f ? -INFINITY : (m + log2f(le)) * 0.69314718055994530942f;
 }
 
-template <int D, int NW, bool DENSE>
-static hipError_t launch_rows(const CacheAttnArgs& a, hipStream_t stream) {
-  const int64_t grid = (int64_t)a.bh * a.ranges * ((a.lq + 32 * NW - 1) / (32 * NW));
-  cache_attn_kernel<D, NW, DENSE><<<grid, 64 * NW, 0, stream>>>(a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.ranges == 1) return e;
+template <int D, int G>
+static hipError_t launch_merge(const CacheAttnArgs& a, hipStream_t stream) {
+  constexpr int RPB = 256 / (D / 8 * G);
   const int64_t rows = (int64_t)a.bh * a.lq;
-  if (NW == 1) {
-    constexpr int RPB = 256 / (D / 8 * 16);
-    cache_merge_kernel<D, 16><<<(rows + RPB - 1) / RPB, 256, 0, stream>>>(a);
-  } else {
-    constexpr int RPB = 256 / (D / 8);
-    cache_merge_kernel<D, 1><<<(rows + RPB - 1) / RPB, 256, 0, stream>>>(a);
-  }
+  if (a.ranges > 1) cache_merge_kernel<D, G><<<(rows + RPB - 1) / RPB, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
-template <int D>
-static hipError_t launch_d(const CacheAttnArgs& a, int waves, bool dense, hipStream_t stream) {
-  if (waves == 1) return dense ? launch_rows<D, 1, true>(a, stream) : launch_rows<D, 1, false>(a, stream);
-  if (waves == 2) return dense ? launch_rows<D, 2, true>(a, stream) : launch_rows<D, 2, false>(a, stream);
-  return dense ? launch_rows<D, 4, true>(a, stream) : launch_rows<D, 4, false>(a, stream);
+template <int D, bool DENSE>
+static hipError_t launch_mode(const CacheAttnArgs& a, int waves, hipStream_t stream) {
+  if (waves == 1) {
+    cache_token_kernel<D, DENSE><<<(int64_t)a.bh * a.ranges, 64, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    return launch_merge<D, 16>(a, stream);
+  }
+  if (waves == 2) cache_attn_kernel<D, 2, DENSE><<<a.grid, 128, 0, stream>>>(a);
+  else cache_attn_kernel<D, 4, DENSE><<<a.grid, 256, 0, stream>>>(a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  return launch_merge<D, 1>(a, stream);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int d, int waves, bool dense, hipStream_t stream) {
-  return d == 128 ? launch_d<128>(a, waves, dense, stream) : launch_d<64>(a, waves, dense, stream);
+  if (d == 128) return dense ? launch_mode<128, true>(a, waves, stream) : launch_mode<128, false>(a, waves, stream);
+  return dense ? launch_mode<64, true>(a, waves, stream) : launch_mode<64, false>(a, waves, stream);
 }
 
 }  // namespace sparstar

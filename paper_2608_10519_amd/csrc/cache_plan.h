@@ -1,39 +1,43 @@
 // How an attention call over the 8-bit cache is cut up (host code): waves per
-// work-group, and ranges of each list.  The kernel (cache_attn.hip) takes the cut
-// through CacheAttnArgs.
+// work-group, ranges of each list, and the order of the work-groups.  The kernels
+// (cache_attn.hip) take the cut through CacheAttnArgs.
 #pragma once
 
 #include <algorithm>
 
-#include "launch.h"
+#include "attn_plan.h"
 
 namespace sparstar {
 
 struct CachePlan {
-  int waves;   // of a work-group, 32 query rows each
-  int ranges;  // of each list's entries
+  int waves;        // of a work-group, 32 query rows each
+  int ranges;       // of each list's entries
+  int rotation;     // as in AttnPlan
+  int spread_bits;
+  int64_t grid;
 };
 
-constexpr int kCacheMaxRanges = 16, kCacheMaxTokenRanges = 64;
+constexpr int kCacheMaxTokenRanges = 64;
 
-// `entries`: key blocks that a list can name.
-inline CachePlan cache_attn_plan(int64_t bh, int64_t lq, int64_t entries, int block, bool dense) {
-  CachePlan p{dense ? (lq <= 64 ? 2 : 4) : block / 32, 1};
+// kv_stride: entries that a list can hold; ignored for the dense call.
+inline CachePlan cache_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
+                                 bool may_split) {
+  const int64_t nk = (lk + block - 1) / block;
   if (lq <= 32) {
     // A few rows stream the cache: single waves, each with its own ring of tiles (32 KB,
     // five to a CU), as many as the chip holds while each has two blocks to read.
-    p.waves = 1;
-    const int64_t want = (256 * 5 + bh - 1) / bh;
-    p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>({want, entries / 2, kCacheMaxTokenRanges}));
+    const int64_t want = (256 * 5 + bh - 1) / bh, entries = dense ? nk : std::min(nk, kv_stride);
+    CachePlan p{1, 1, 0, 0, 0};
+    if (may_split) p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>({want, entries / 2, kCacheMaxTokenRanges}));
+    p.grid = bh * p.ranges;
     return p;
   }
-  const int64_t groups = bh * ((lq + 32 * p.waves - 1) / (32 * p.waves)), held = 256 * 8 / p.waves;
-  while (p.ranges < kCacheMaxRanges && groups * p.ranges < 2 * held && entries >= 16 * p.ranges) p.ranges *= 2;
-  return p;
+  const AttnPlan p = attn_plan(bh, lq, lk, d, block, kv_stride, dense, may_split && nk >= kSplits);
+  return {p.group_rows / 32, p.ranges, p.rotation, p.spread_bits, p.grid};
 }
 
 inline size_t cache_part_o_bytes(int64_t rows, int d, int ranges) {
-  return (size_t(rows * d) * ranges * sizeof(float) + 255) & ~size_t(255);
+  return (size_t(rows * d) * ranges * 2 + 255) & ~size_t(255);
 }
 
 inline size_t cache_attn_workspace(int64_t rows, int d, int ranges) {

@@ -197,8 +197,11 @@ struct CacheAttnArgs {
   int bh, heads, block, n_q, stride;
   float scale_log2;
   int ranges;                      // ranges of each list; 1: results go out at once
-  float* part_o;                   // [ranges, BH, Lq, D]: unnormalised P V
-  float* part_meta;                // [ranges, BH, Lq, 4]: running max (log2 units), row sums of the bf16 and the fp32 P
+  uint16_t* part_o;                // [ranges, BH, Lq, D] fp16: unnormalised P V times 2^-e per row
+  float* part_meta;                // [ranges, BH, Lq, 4]: running max (log2 units), row sums of the bf16 and the fp32 P, e
+  int rotation;                    // work-groups in flight per XCD, for the start of each list; 0: start at its head
+  int spread_bits;                 // log2 of the XCDs that share a (head, range) pair
+  int64_t grid;                    // work-groups (launcher only)
 };
 
 hipError_t launch_pool(const PoolArgs& a, int d, int block, hipStream_t stream);
