@@ -319,31 +319,29 @@ void cache_token_kernel(CacheAttnArgs a) {
 //
 // What bounds it is the VALU: a 32x32x16 MFMA takes the time of 7.7 VALU instructions
 // (two waves per SIMD), the softmax takes 4.2 of those per MFMA at D = 128, and turning
-// every K and V operand into bf16 takes 4 more in each wave.  So V is turned into bf16
-// once per work-group: each wave takes its share of a tile from LDS and puts it back in
-// the layout of the transpose read (0.5 conversions per MFMA and wave with four waves, 1
-// with two); K is converted as it is read (2 per MFMA).  Products of codes would need no
-// conversion of K, with Q as the sum of two e4m3 numbers: but v_mfma_f32_32x32x64_f8f6f4
-// aligns the products of eight columns to the largest of them with 13 bits, which was
-// measured to cost up to 8e-4 of the lse.
+// every K and V operand into bf16 would take 4 more in each wave.  So both are turned into
+// bf16 once per work-group, on the way into LDS: a wave loads its share of a raw tile into
+// registers two steps ahead, converts it and stores it, K in the layout of row reads and V
+// in that of the transpose read (1 conversion per MFMA and wave with four waves, 2 with
+// two).  Products of codes would need no conversion of K, with Q as the sum of two e4m3
+// numbers; but v_mfma_f32_32x32x64_f8f6f4 aligns the products of eight columns to the
+// largest of them with 13 bits, which cost up to 8e-4 of the lse.
 //
 // Step t: S of tile t + 1 and P V of tile t - 1 on the matrix cores, the softmax of tile t
-// spread evenly under them, V of tile t converted.  One barrier per step, behind which the
-// converted tile and the next raw tiles can be read, and the raw ones that were read are
-// overwritten; loads have two steps to land.
+// spread evenly under them, K of tile t + 2 and V of tile t converted.  One barrier per
+// step, P MFMAs before its end, behind which the converted tiles can be read.
 // The softmax keeps a running max that is only refreshed when some lane's sum of a tile's
 // P exceeds 2^8 (attn_fwd.hip); the row sum of the bf16 P comes from 4x4x4 MFMAs.
 template <int D, int NW>
 struct CachePipe : CacheCfg<D> {
   using B = CacheCfg<D>;
-  static constexpr int N = 4 / NW;              // direct loads per wave and raw tile
-  static constexpr int RING = 3;                // raw tiles in LDS, K and V each
   static constexpr int NA = B::KT * B::DS;      // MFMAs of S
   static constexpr int NB = 2 * B::KT * B::DT;  // MFMAs of P V
   static constexpr int NE = 16 * B::KT;         // elements of S per lane
   static constexpr int EPU = NE / 16;           // elements per MFMA
-  static constexpr int VTILE = B::KB * D;       // elements of a converted tile
-  static constexpr int CV = 4 / NW;             // 16-code pieces of V that a lane converts
+  static constexpr int CT = B::KB * D;          // elements of a converted tile
+  static constexpr int CV = 4 / NW;             // 16-code pieces of a tile that a lane converts
+  static constexpr int P = 4, PV = 6;           // MFMAs between a K (V) operand's read and its use
   static_assert(NA == 8 && NB == 8, "a step is 16 MFMAs");
 };
 
@@ -357,14 +355,30 @@ __device__ __forceinline__ void static_for(F&& f) {
   static_for(f, std::make_integer_sequence<int, N>{});
 }
 
+// A raw buffer over `bytes` bytes, in scalar registers.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint8_t* p, uint32_t bytes) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)hi << 32 | lo), 0,
+                                           __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
+}
+
+// A barrier that makes LDS writes visible and lets LDS reads end, and waits for no load.
+__device__ __forceinline__ void publish_lds() {
+  __builtin_amdgcn_s_waitcnt((63 & 15) | ((63 >> 4) << 14) | (7 << 4));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 template <int D, int NW, bool DENSE>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void cache_attn_kernel(CacheAttnArgs a) {
   using C = CachePipe<D, NW>;
   constexpr int ROWS = 32 * NW;
-  __shared__ __attribute__((aligned(1024))) uint8_t kr[C::RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint8_t vr[C::RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t vb[2][C::VTILE];
+  __shared__ __attribute__((aligned(1024))) uint16_t kb[2][C::CT];
+  __shared__ __attribute__((aligned(1024))) uint16_t vb[2][C::CT];
 
   // Work item: as in attn_fwd.hip, the query groups of a (head, range) pair are dealt out
   // to 2^spread_bits XCDs, each of which runs its share of a pair after the other.
@@ -383,7 +397,7 @@ void cache_attn_kernel(CacheAttnArgs a) {
     pair = unit >> a.spread_bits;
     qg = (int)((gi << a.spread_bits) + (unit & ((1u << a.spread_bits) - 1)));
   }
-  if (pair >= (uint32_t)(a.bh * a.ranges) || qg >= (int)n_g) return;  // uniform: past the last unit or group
+  if (pair >= (uint32_t)a.bh * (uint32_t)a.ranges || qg >= (int)n_g) return;  // uniform: past the last unit or group
   const int64_t bh = pair / (uint32_t)a.ranges;
   const int range = (int)(pair - (uint32_t)bh * (uint32_t)a.ranges);
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -397,14 +411,13 @@ void cache_attn_kernel(CacheAttnArgs a) {
   }
   const int n_blk = (int)((len + a.block - 1) / a.block);
 
-  // ---- Q as the B operand of S^T = K Q^T.  A 16-byte read of a K row feeds two k-steps, so
-  // step 2 i + j covers columns 32 i + 16 h + 8 j + (0..7).
+  // ---- Q as the B operand of S^T = K Q^T: Q[q][16 s + 8 h .. +7]
   const int64_t row = (int64_t)qg * ROWS + wave * 32 + l32;
   const bool row_ok = row < a.lq;
   bf16x8 qf[C::DS];
 #pragma unroll
   for (int s = 0; s < C::DS; ++s) {
-    const uint16_t* p = a.q + (bh * a.lq + (row_ok ? row : 0)) * D + 32 * (s / 2) + 16 * hh + 8 * (s % 2);
+    const uint16_t* p = a.q + (bh * a.lq + (row_ok ? row : 0)) * D + 16 * s + 8 * hh;
     const uint4 u = row_ok ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
     qf[s] = __builtin_bit_cast(bf16x8, u);
   }
@@ -464,47 +477,54 @@ void cache_attn_kernel(CacheAttnArgs a) {
     return Tile{b < 0 ? -1 : b * SUB + j % SUB, __builtin_amdgcn_readlane(sreg, e - lbase)};
   };
 
-  // ---- raw tiles: K rows with their chunks permuted (read by rows), V as it is
-  // (the instruction adds 1024 i to the i-th load of a wave)
-  const uint32_t voffs[2] = {(uint32_t)(1024 * C::N * wave + 16 * lane), (uint32_t)(1024 * C::N * wave + 16 * lane)};
-  uint32_t koffs[C::N];
-#pragma unroll
-  for (int i = 0; i < C::N; ++i) {
-    const int r = C::RPD * (C::N * wave + i) + lane / C::CPR;
-    koffs[i] = (uint32_t)(r * C::RB + 16 * ((lane % C::CPR) ^ cache_swz<D>(r)) - 1024 * i);
-  }
-  const uint32_t kr0 = lds_addr(kr), vr0 = lds_addr(vr);
+  // ---- raw tiles: the lane's 16-code pieces at byte src + 1024 i of a tile.  Each tile gets
+  // its own descriptor, so that rows past the sequence's end arrive as zeros.
   const uint8_t* const kbase = a.k_cache + bh * a.cap * D;
   const uint8_t* const vbase = a.v_cache + bh * a.cap * D;
   const uint32_t n_whole = (uint32_t)(len / C::KB), last_bytes = (uint32_t)(len % C::KB) * C::RB;
-  auto issue = [&](const uint8_t* base, int tile, uint32_t slot, const uint32_t* offs) {
+  const int src = 1024 * C::CV * wave + 16 * lane;
+  auto load_raw = [&](const uint8_t* base, int tile, uint4 (&u)[C::CV]) {
     const uint32_t bytes = (uint32_t)tile < n_whole ? C::TILE : ((uint32_t)tile == n_whole ? last_bytes : 0u);
-    const uint32_t m0 = __builtin_amdgcn_readfirstlane(slot + (uint32_t)(C::N * wave) * 1024u);
-    dma_tile<C::N>(m0, offs, raw_rsrc(base + (int64_t)tile * C::TILE, bytes));
+    const auto rs = tile_rsrc(base + (int64_t)tile * C::TILE, bytes);
+#pragma unroll
+    for (int i = 0; i < C::CV; ++i)
+      u[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, src + 1024 * i, 0, 0));
   };
 
-  // ---- per-lane LDS offsets
-  uint32_t koff[C::DS / 2];  // K row l32, chunk 2 i + h
+  // ---- converted tiles: rows of 2 D bytes whose 16-byte chunks are permuted as in
+  // attn_fwd.hip, chunk c of K row r at c ^ kswz(r), of V row r at c ^ vswz(r)
+  constexpr int CRB = 2 * D, CRPB = 256 / CRB, CCPR = D / 8;
+  auto kswz = [](int r) { return (r / CRPB) % CCPR; };
+  auto vswz = [](int r) { return (((r / CRPB) & 3) << 2) & (CCPR - 1); };
+  uint32_t koff[C::DS];  // K row l32, chunk 2 s + h
 #pragma unroll
-  for (int i = 0; i < C::DS / 2; ++i) koff[i] = (uint32_t)(l32 * C::RB + 16 * ((2 * i + hh) ^ cache_swz<D>(l32)));
-  // converted V: rows of 2 D bytes, 16-byte chunk c of row r at c ^ vswz(r), as attn_fwd.hip has it
-  constexpr int VRB = 2 * D, VRPB = 256 / VRB, VCPR = D / 8;
-  auto vswz = [](int r) { return (((r / VRPB) & 3) << 2) & (VCPR - 1); };
+  for (int s = 0; s < C::DS; ++s) koff[s] = (uint32_t)(l32 * CRB + 16 * ((2 * s + hh) ^ kswz(l32)));
   uint32_t voff[C::DT];  // transpose read: rows 4 h + (0..3), columns 32 t + l % 32
   {
     const int sl = lane & 15, r = 4 * hh + (sl >> 2);
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
-      voff[t] = (uint32_t)(r * VRB + 16 * ((4 * t + 2 * (lane >> 4 & 1) + ((sl & 3) >> 1)) ^ vswz(r)) + 8 * (sl & 1));
+      voff[t] = (uint32_t)(r * CRB + 16 * ((4 * t + 2 * (lane >> 4 & 1) + ((sl & 3) >> 1)) ^ vswz(r)) + 8 * (sl & 1));
   }
-  // what the lane converts: 16 codes from byte cv_src + 1024 i of the tile; they go to two
-  // neighbouring chunks (8 or 16 rows further per i, where the permutation is the same)
-  const uint32_t cv_src = (uint32_t)(16 * lane + 1024 * C::CV * wave);
-  uint32_t cv_dst;
+  // Where the lane's pieces go: to two neighbouring chunks, 8 (D = 64: 16) rows further per
+  // i, which moves kswz by 8 chunks of 16 (D = 128) or not at all, and leaves vswz as it is.
+  uint32_t kdst, vdst;
   {
-    const int r = (int)cv_src / C::RB, c = (int)cv_src % C::RB / 16;
-    cv_dst = (uint32_t)(r * VRB + 16 * ((2 * c) ^ vswz(r)));
+    const int r = src / C::RB, c = 2 * (src % C::RB / 16);
+    kdst = (uint32_t)(r * CRB + 16 * (c ^ kswz(r)));
+    vdst = (uint32_t)(r * CRB + 16 * (c ^ vswz(r)));
   }
+  auto convert = [&](uint4 u, int byte, char* tile, uint32_t dst) {
+    const float sc = __uint_as_float((uint32_t)(byte & 255) << 23);
+    *reinterpret_cast<bf16x8*>(tile + dst) = decode8(make_uint2(u.x, u.y), sc);
+    *reinterpret_cast<bf16x8*>(tile + (dst ^ 16u)) = decode8(make_uint2(u.z, u.w), sc);
+  };
+  auto convert_k = [&](uint4 u, int i, int s, int buf) {
+    convert(u, s, reinterpret_cast<char*>(kb[buf]) + 2048 * i, D == 128 ? kdst ^ (uint32_t)(128 * (i % 2)) : kdst);
+  };
+  auto convert_v = [&](uint4 u, int i, int s, int buf) {
+    convert(u, s >> 8, reinterpret_cast<char*>(vb[buf]) + 2048 * i, vdst);
+  };
 
   const s16x4 one4 = {0x3f80, 0x3f80, 0x3f80, 0x3f80};  // bf16 1.0
   auto mask_tile = [&](f32x16* x, int tile) {
@@ -535,45 +555,36 @@ void cache_attn_kernel(CacheAttnArgs a) {
   float m_run = -INFINITY, l_run = 0.f, le_run = 0.f;  // max in the log2 domain; sums of the lane's half of the keys
 
   if (ntiles > 0) {
-    // K operands: 16-byte piece o of a tile's rows holds those of MFMAs 2 o and 2 o + 1 of S
-    constexpr int NK = C::NA / 2, KPT = NK / C::KT;
-    auto read_k = [&](int o, uint32_t slot) -> uint4 {
-      return *reinterpret_cast<const uint4*>(&kr[0][0] + slot + o / KPT * 32 * C::RB + koff[o % KPT]);
+    // K operand of MFMA n = kt DS + s of S
+    auto read_k = [&](int n, int buf) -> bf16x8 {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(kb[buf]) +
+                                                                        koff[n % C::DS] + n / C::DS * 32 * CRB));
     };
-    auto k_operand = [&](uint4 u, int j, float sc) { return decode8(j == 0 ? make_uint2(u.x, u.y) : make_uint2(u.z, u.w), sc); };
-    auto k_scale = [](int s) { return __uint_as_float((uint32_t)(s & 255) << 23); };
     // V^T operand of P V: step m = (2 kt + half) DT + dt
     auto read_v = [&](int m, int buf) -> bf16x8 {
       typedef __attribute__((address_space(3))) uint16_t lds16;
-      const lds16* p = (const lds16*)vb[0] + (voff[m % C::DT] / 2 + 16 * (m / C::DT) * D + buf * C::VTILE);
+      const lds16* p = (const lds16*)vb[0] + (voff[m % C::DT] / 2 + 16 * (m / C::DT) * D + buf * C::CT);
       const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
       const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 8 * D));
       return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto convert = [&](uint4 u, float sc, int i, uint16_t* tile) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t x = k == 0 ? u.x : u.z, y = k == 0 ? u.y : u.w;
-        uint4 r;
-        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, sc, false));
-        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, sc, true));
-        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, sc, false));
-        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, sc, true));
-        *reinterpret_cast<uint4*>(reinterpret_cast<char*>(tile) + 2048 * i + (cv_dst ^ (uint32_t)(16 * k))) = r;
-      }
-    };
-    // ---- prologue: raw K of tiles 0..2, V of 0..1; S of tile 0
+    // ---- prologue: K of tiles 0 and 1 converted, S of tile 0, raw tiles in flight
     load_batch(0);
     Tile t0 = fetch(0), t1 = fetch(1), t2 = fetch(2), t3 = fetch(3);
-    issue(kbase, t0.t, kr0 + 0 * C::TILE, koffs);
-    issue(kbase, t1.t, kr0 + 1 * C::TILE, koffs);
-    issue(vbase, t0.t, vr0 + 0 * C::TILE, voffs);
-    issue(kbase, t2.t, kr0 + 2 * C::TILE, koffs);
-    issue(vbase, t1.t, vr0 + 1 * C::TILE, voffs);
-    issue(vbase, t2.t, vr0 + 2 * C::TILE, voffs);
+    uint4 kraw[2][C::CV], vraw[2][C::CV];  // of tiles t + 2 and t + 3, t and t + 1
+    load_raw(kbase, t0.t, kraw[0]);
+    load_raw(kbase, t1.t, kraw[1]);
+    load_raw(vbase, t0.t, vraw[0]);
+    load_raw(vbase, t1.t, vraw[1]);
+#pragma unroll
+    for (int i = 0; i < C::CV; ++i) {
+      convert_k(kraw[0][i], i, t0.s, 0);
+      convert_k(kraw[1][i], i, t1.s, 1);
+    }
+    load_raw(kbase, t2.t, kraw[0]);
+    load_raw(kbase, t3.t, kraw[1]);
     // "P V of tile -1" multiplies zeros
-    for (int i = threadIdx.x; i < C::VTILE / 8; i += 64 * NW) reinterpret_cast<uint4*>(vb[1])[i] = make_uint4(0, 0, 0, 0);
-    wait_vmcnt<0>();
+    for (int i = threadIdx.x; i < C::CT / 8; i += 64 * NW) reinterpret_cast<uint4*>(vb[1])[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     f32x16 s[C::KT];  // S^T of tile t
 #pragma unroll
@@ -582,38 +593,33 @@ void cache_attn_kernel(CacheAttnArgs a) {
       for (int e = 0; e < 16; ++e) s[kt][e] = 0.f;
     static_for<C::NA>([&](auto nc) {
       constexpr int n = decltype(nc)::value, kt = n / C::DS;
-      s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(read_k(n / 2, 0u), n % 2, k_scale(t0.s)), qf[n % C::DS],
-                                                      s[kt], 0, 0, 0);
+      s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(n, 0), qf[n % C::DS], s[kt], 0, 0, 0);
     });
     if ((uint32_t)t0.t >= n_whole) mask_tile(s, t0.t);
     m_run = half_swap_max(tile_max(s)) * sl2;  // O and the sums are still zero
-    u32x8 pp[C::KT];  // bf16 pairs of P^T of tile t - 1
+    u32x8 pp[C::KT];                           // bf16 pairs of P^T of tile t - 1
 #pragma unroll
     for (int kt = 0; kt < C::KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 8; ++i) pp[kt][i] = 0u;
-    __syncthreads();  // slot 0 of K is free
-    issue(kbase, t3.t, kr0, koffs);
+    bf16x8 ahead[C::P];                        // K operands of the next MFMAs
+#pragma unroll
+    for (int i = 0; i < C::P; ++i) ahead[i] = read_k(i, 1);
+    __syncthreads();  // the first step overwrites K of tile 0
 
-    // Raw tile j lies in slot j % RING.  At the barrier of step t the loads of K(t + 2) and
-    // V(t + 1) have landed; V(t + 3) and K(t + 4) follow into the slots of V(t) and K(t + 1).
     int j = 0;
-    uint32_t slot0 = 0, slot1 = C::TILE;  // of raw tiles t and t + 1, in bytes
     auto step = [&](auto tc) {
-      constexpr int T = decltype(tc)::value;  // t mod 2
-      constexpr int vt = (T + 1) % 2;               // buffer of V(t - 1)
-      uint16_t* const vt_next = vb[T % 2];          // V(t)
+      // t mod 2: the buffer of K(t), which K(t + 2) takes, and of V(t)
+      constexpr int T = decltype(tc)::value, U = 1 - T;
+      constexpr int X = C::NA + C::NB - C::P;  // MFMA before which the barrier stands
       f32x16 sn[C::KT];
       u32x8 pk[C::KT];
-      uint4 kop[NK];
-      bf16x8 vop[C::NB];
-      uint4 raw[C::CV];
-#pragma unroll
-      for (int n = 0; n < NK; ++n) kop[n] = read_k(n, slot1);
+      bf16x8 kop[C::NA + C::P], vop[C::NB];
       float x[C::NE], p[C::NE], se = 0.f;
       f32x4 st4 = {0.f, 0.f, 0.f, 0.f};
       const float neg_m = m_run == -INFINITY ? INFINITY : -m_run;  // (no key seen yet: takes the exact path)
-      const float vsc = __uint_as_float((uint32_t)(t0.s >> 8) << 23), ksc = k_scale(t1.s);
+#pragma unroll
+      for (int i = 0; i < C::P; ++i) kop[i] = ahead[i];
       auto row_sum = [&](auto ic) {  // adds pairs i - 1 and i of P
         constexpr int i = decltype(ic)::value;
         const uint2 u = make_uint2(pk[i / 8][i % 8 - 1], pk[i / 8][i % 8]);
@@ -639,53 +645,43 @@ void cache_attn_kernel(CacheAttnArgs a) {
         prob(std::integral_constant<int, e + 1>{});
         se = e == 0 ? p[0] : se + p[e];
         asm volatile("" : "+v"(se));
-        if constexpr (e % 2 == 1) {
-          pk[e / 16][e % 16 / 2] = pack2_bf16(p[e - 1], p[e]);
-        }
-      };
-      auto unit = [&](auto uc) {  // the softmax under one MFMA
-        static_for<C::EPU>([&](auto k) {
-          element(std::integral_constant<int, decltype(uc)::value * C::EPU + decltype(k)::value>{});
-        });
+        if constexpr (e % 2 == 1) pk[e / 16][e % 16 / 2] = pack2_bf16(p[e - 1], p[e]);
       };
       logit(std::integral_constant<int, 0>{});
       logit(std::integral_constant<int, 1>{});
       prob(std::integral_constant<int, 0>{});
       __builtin_amdgcn_sched_barrier(0);
-      // ---- S of tile t + 1; each operand is converted one MFMA ahead
-      bf16x8 kb = k_operand(kop[0], 0, ksc);
-      static_for<C::NA>([&](auto nc) {
-        constexpr int n = decltype(nc)::value, kt = n / C::DS;
-        if constexpr (n % C::DS == 0)
+      static_for<C::NA + C::NB>([&](auto nc) {
+        constexpr int n = decltype(nc)::value;
+        if constexpr (n < C::NA) {  // S of tile t + 1
+          constexpr int kt = n / C::DS;
+          if constexpr (n % C::DS == 0)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sn[kt][e] = 0.f;
-        sn[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb, qf[n % C::DS], sn[kt], 0, 0, 0);
-        if constexpr (n + 1 < C::NA) kb = k_operand(kop[(n + 1) / 2], (n + 1) % 2, ksc);
-        if constexpr (n >= 4) vop[n - 4] = read_v(n - 4, vt);
-        if constexpr (n == C::NA - 1)
-#pragma unroll
-          for (int k = 0; k < C::CV; ++k) raw[k] = *reinterpret_cast<const uint4*>(&vr[0][0] + slot0 + cv_src + 1024 * k);
-        unit(std::integral_constant<int, n>{});
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      // ---- P V of tile t - 1, while V(t) is converted
-      static_for<C::NB>([&](auto mc) {
-        constexpr int m = decltype(mc)::value, kt = m / C::DT / 2, half = m / C::DT % 2, dt = m % C::DT;
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[m], pack_half(pp[kt], half), acc[dt], 0, 0, 0);
-        if constexpr (m + 4 < C::NB) vop[m + 4] = read_v(m + 4, vt);
-        if constexpr (m < C::CV) convert(raw[m], vsc, m, vt_next);
-        unit(std::integral_constant<int, 8 + m>{});
+            for (int e = 0; e < 16; ++e) sn[kt][e] = 0.f;
+          sn[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[n], qf[n % C::DS], sn[kt], 0, 0, 0);
+        } else {  // P V of tile t - 1
+          constexpr int m = n - C::NA, kt = m / C::DT / 2, half = m / C::DT % 2, dt = m % C::DT;
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[m], pack_half(pp[kt], half), acc[dt], 0, 0, 0);
+        }
+        // the converted tiles can be read behind the barrier, those of the step before
+        // overwritten
+        if constexpr (n == X - 1) publish_lds();
+        constexpr int rk = n + C::P, rv = n + C::PV - C::NA;
+        if constexpr (rk < C::NA) kop[rk] = read_k(rk, U);
+        if constexpr (rk >= C::NA + C::NB) kop[rk - C::NB] = read_k(rk - C::NA - C::NB, T);
+        if constexpr (rv >= 0 && rv < C::NB) vop[rv] = read_v(rv, U);
+        // K of tile t + 2 and V of tile t, a piece at a time; their registers take the raw
+        // pieces of two tiles on
+        if constexpr (n % 2 == 0 && n / 2 < C::CV) convert_k(kraw[T][n / 2], n / 2, t2.s, T);
+        if constexpr (n % 2 == 0 && n >= 4 && n / 2 - 2 < C::CV) convert_v(vraw[T][n / 2 - 2], n / 2 - 2, t0.s, T);
+        static_for<C::EPU>([&](auto k) { element(std::integral_constant<int, n * C::EPU + decltype(k)::value>{}); });
         __builtin_amdgcn_sched_barrier(0);
       });
       static_for<C::NE / 4>([&](auto k) { row_sum(std::integral_constant<int, 2 * decltype(k)::value + 1>{}); });
       float st = st4[0];
       const Tile t4 = fetch(j + 4);
-      wait_loads_and_lds<2 * C::N>();  // (all but the youngest two, V(t + 2) and K(t + 3))
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      issue(vbase, t3.t, vr0 + slot0, voffs);
-      issue(kbase, t4.t, kr0 + slot1, koffs);
+      load_raw(vbase, t2.t, vraw[T]);
+      load_raw(kbase, t4.t, kraw[T]);
 
       // A lane's sum of its P stays <= 2^8 whenever every p does; otherwise the exact path:
       // the tile's max, a rescale of O (tiles up to t - 1) and both sums, and P again.
@@ -730,12 +726,12 @@ void cache_attn_kernel(CacheAttnArgs a) {
         s[kt] = sn[kt];
         pp[kt] = pk[kt];
       }
+#pragma unroll
+      for (int i = 0; i < C::P; ++i) ahead[i] = kop[C::NA + i];
       t0 = t1;
       t1 = t2;
       t2 = t3;
       t3 = t4;
-      slot0 = slot1;
-      slot1 = slot1 == 2 * C::TILE ? 0 : slot1 + C::TILE;
     };
     while (true) {
       step(std::integral_constant<int, 0>{});
@@ -743,12 +739,11 @@ void cache_attn_kernel(CacheAttnArgs a) {
       step(std::integral_constant<int, 1>{});
       if (++j >= ntiles) break;
     }
-    // P V of the last tile, which the last step converted
+    // P V of the last tile, which the last step converted and published
 #pragma unroll
     for (int m = 0; m < C::NB; ++m)
       acc[m % C::DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           read_v(m, (ntiles - 1) % 2), pack_half(pp[m / C::DT / 2], m / C::DT % 2), acc[m % C::DT], 0, 0, 0);
-    wait_vmcnt<0>();  // loads past the end of the list still write LDS
   }
   store_rows<D>(a, bh, row, range, acc, m_run, half_swap_sum(l_run), half_swap_sum(le_run), hh);
 }
