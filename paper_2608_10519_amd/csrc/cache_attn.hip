@@ -116,12 +116,15 @@ __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, i
 // ---- up to 32 query rows: one wave per (head, range of the list), with a ring of tiles of
 // its own and no barrier.  S^T = K Q^T and O^T += V^T P^T as in attn_fwd.hip, with the
 // operands turned into bf16 in registers; mostly empty products, but the matrix cores
-// could take 34 TB/s of codes this way.
+// could take 34 TB/s of codes this way.  A lone wave needs 0.7 us per tile, so what counts
+// is how many there are: two tiles of K and V in LDS (16 KB) let ten run on a CU, and the
+// call cuts its lists into about 1,024 ranges, four to a CU.  24 heads of 144,512 rows: 160
+// us with two tiles, 177 with three or four; 5.5 TB/s, of some 6.2 that reading reaches.
 template <int D, bool DENSE>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(3, 3)))
 void cache_token_kernel(CacheAttnArgs a) {
   using C = CacheCfg<D>;
-  constexpr int RING = 4;
+  constexpr int RING = 2;
   __shared__ __attribute__((aligned(1024))) uint8_t ks[RING][C::TILE];
   __shared__ __attribute__((aligned(1024))) uint8_t vs[RING][C::TILE];
   const int64_t bh = blockIdx.x / a.ranges;
@@ -750,47 +753,56 @@ void cache_attn_kernel(CacheAttnArgs a) {
 
 // Joins the ranges of one row: with M = max_r m_r and w_r = 2^(m_r - M),
 // O = sum w_r 2^e_r A_r / sum w_r l_r and lse = ln 2 (M + log2 sum w_r le_r).  D / 8 threads
-// per row and G groups of them, each over every G-th range.
+// per row and G groups of them, each over every G-th range; the groups' own sums are joined
+// the same way through LDS.
 template <int D, int G>
 __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs a) {
   constexpr int LPR = D / 8, RPB = 256 / (LPR * G);
-  __shared__ float red[G][RPB][LPR][8];
+  __shared__ float red[G][RPB][LPR][8], meta[G][RPB][3];
   const int c = threadIdx.x % LPR, g = threadIdx.x / LPR % G, rb = threadIdx.x / (LPR * G);
   const int64_t rows = (int64_t)a.bh * a.lq, row = (int64_t)blockIdx.x * RPB + rb;
   const bool ok = row < rows;
-  float m = -INFINITY, l = 0.f, le = 0.f;
-  const float4* meta = reinterpret_cast<const float4*>(a.part_meta);
-  if (ok)
-    for (int r = 0; r < a.ranges; ++r) {
-      const float4 x = meta[(int64_t)r * rows + row];
-      const float mn = fmaxf(m, x.x);
-      if (x.y != 0.f) {
-        const float s = __builtin_amdgcn_exp2f(m - mn), t = __builtin_amdgcn_exp2f(x.x - mn);
-        l = l * s + x.y * t;
-        le = le * s + x.z * t;
-        m = mn;
-      }
-    }
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (ok)
+  float m = -INFINITY, l = 0.f, le = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (ok) {
+#pragma unroll 4
     for (int r = g; r < a.ranges; r += G) {
       const int64_t p = (int64_t)r * rows + row;
-      const float4 x = meta[p];
+      const float4 x = reinterpret_cast<const float4*>(a.part_meta)[p];
       const f16x8 u = *reinterpret_cast<const f16x8*>(reinterpret_cast<const _Float16*>(a.part_o) + p * D + 8 * c);
       if (x.y == 0.f) continue;  // no key seen; NaN passes on
-      const float t = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(x.x - m), (int)x.w);
+      const float mn = fmaxf(m, x.x), s = __builtin_amdgcn_exp2f(m - mn), t = __builtin_amdgcn_exp2f(x.x - mn);
+      const float w = __builtin_amdgcn_ldexpf(t, (int)x.w);
+      l = l * s + x.y * t;
+      le = le * s + x.z * t;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(t, (float)u[e], acc[e]);
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, (float)u[e], acc[e] * s);
+      m = mn;
     }
+  }
   if constexpr (G > 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[g][rb][c][e] = acc[e];
+    if (c == 0) meta[g][rb][0] = m, meta[g][rb][1] = l, meta[g][rb][2] = le;
     __syncthreads();
     if (g != 0) return;
+    float mm = m;
 #pragma unroll
-    for (int i = 1; i < G; ++i)
+    for (int i = 1; i < G; ++i) mm = fmaxf(mm, meta[i][rb][0]);
+    // (a group without keys has m = -inf, and so has mm if none has any)
+    auto weight = [&](float x) { return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - mm); };
+    float s = weight(m);
+    l = l == 0.f ? 0.f : l * s, le = le == 0.f ? 0.f : le * s;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += red[i][rb][c][e];
+    for (int e = 0; e < 8; ++e) acc[e] = acc[e] * s;
+#pragma unroll
+    for (int i = 1; i < G; ++i) {
+      s = weight(meta[i][rb][0]);
+      l = fmaf(meta[i][rb][1], s, l);
+      le = fmaf(meta[i][rb][2], s, le);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(red[i][rb][c][e], s, acc[e]);
+    }
+    m = mm;
   }
   if (!ok) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;

@@ -17,16 +17,19 @@ struct CachePlan {
   int64_t grid;
 };
 
-constexpr int kCacheMaxTokenRanges = 64;
+constexpr int kCacheMaxTokenRanges = 256;
 
 // kv_stride: entries that a list can hold; ignored for the dense call.
 inline CachePlan cache_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
                                  bool may_split) {
   const int64_t nk = (lk + block - 1) / block;
   if (lq <= 32) {
-    // A few rows stream the cache: single waves, each with its own ring of tiles (32 KB,
-    // five to a CU), as many as the chip holds while each has two blocks to read.
-    const int64_t want = (256 * 5 + bh - 1) / bh, entries = dense ? nk : std::min(nk, kv_stride);
+    // A few rows stream the cache: single waves, four to a CU (with more, some CUs get five or
+    // six and the call waits for them: 1,792 waves 166 us, 2,560 197, 1,024 172 for two
+    // sequences of 24 heads, 84,032 and 67,226 rows; of 24 heads, 8,000 rows, 24, 24 and 18).
+    // A wave reads two blocks at least, and a row's ranges are bounded, since joining them
+    // costs as much as reading them (one head of 144,512 rows: 256 ranges 31 us, 1,024 49).
+    const int64_t want = 1024 / bh, entries = dense ? nk : std::min(nk, kv_stride);
     CachePlan p{1, 1, 0, 0, 0};
     if (may_split) p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>({want, entries / 2, kCacheMaxTokenRanges}));
     p.grid = bh * p.ranges;
