@@ -18,9 +18,6 @@
 //
 // The key groups find their query blocks in a bit matrix, one bit per (key block,
 // query block), that a small kernel builds from the lists.
-#include <type_traits>
-#include <utility>
-
 #include "attn_device.h"
 
 namespace sparstar {
@@ -154,10 +151,10 @@ __device__ __forceinline__ void publish() {
 // unscaled logit is offset by) then [32] of -delta, padded to whole query blocks: a row past Lq,
 // and one that saw no key, gets -inf and 0, which makes its P and dS zero.
 template <int D>
-__global__ __launch_bounds__(256) void attn_bwd_stats_kernel(BwdArgs a) {
+__device__ __forceinline__ void row_stats(const BwdArgs& a, int64_t group) {
   constexpr int LPR = D / 8, RPW = 256 / LPR;
   const int64_t rows_pad = (int64_t)a.n_q * a.block;
-  const int64_t i = (int64_t)blockIdx.x * RPW + threadIdx.x / LPR;
+  const int64_t i = group * RPW + threadIdx.x / LPR;
   if (i >= a.bh * rows_pad) return;
   const int64_t bh = i / rows_pad, t = i - bh * rows_pad;
   const int c = threadIdx.x % LPR;
@@ -194,38 +191,40 @@ __global__ __launch_bounds__(256) void attn_bwd_stats_kernel(BwdArgs a) {
 // ---- the bit matrix: word w of key block j holds, bit i, whether query block
 // 32 w + i lists j.  One work-group per word column and up to kBitsChunk key blocks.
 constexpr int kBitsChunk = 8192;
-__global__ __launch_bounds__(1024) void attn_bwd_bits_kernel(BwdArgs a) {
-  __shared__ uint32_t bits[kBitsChunk];
-  const int64_t bh = blockIdx.x / a.n_words;
-  const int word = (int)(blockIdx.x - bh * a.n_words);
-  const int lo = (int)blockIdx.y * kBitsChunk;
+__device__ __forceinline__ void list_bits(const BwdArgs& a, int64_t column, int chunk, uint32_t* bits) {
+  const int64_t bh = column / a.n_words;
+  const int word = (int)(column - bh * a.n_words);
+  const int lo = chunk * kBitsChunk;
   const int hi = a.n_k - lo < kBitsChunk ? a.n_k : lo + kBitsChunk;
-  for (int j = threadIdx.x; j < hi - lo; j += 1024) bits[j] = 0u;
+  for (int j = threadIdx.x; j < hi - lo; j += 256) bits[j] = 0u;
   __syncthreads();
   const int lane = threadIdx.x % 64;
-  for (int i = threadIdx.x / 64; i < 32; i += 16) {
+  for (int i = threadIdx.x / 64; i < 32; i += 4) {
     const int qb = 32 * word + i;
     if (qb >= a.n_q) break;
     const int64_t r = bh * a.n_q + qb;
     int n = a.kv_num_blocks[r];
     n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
+#pragma unroll 4
     for (int e = lane; e < n; e += 64) {
       const int j = a.kv_indices[r * a.stride + e];
       if (j >= lo && j < hi) atomicOr(&bits[j - lo], 1u << i);
     }
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < hi - lo; j += 1024) a.bits[(bh * a.n_k + lo + j) * a.n_words + word] = bits[j];
+  for (int j = threadIdx.x; j < hi - lo; j += 256) a.bits[(bh * a.n_k + lo + j) * a.n_words + word] = bits[j];
 }
 
-// f(0), .., f(N - 1) with each index a compile-time constant
-template <class F, int... I>
-__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void static_for(F&& f) {
-  static_for(f, std::make_integer_sequence<int, N>{});
+// Both in one launch: the first `stat_groups` work-groups take the rows.
+template <int D>
+__global__ __launch_bounds__(256) void attn_bwd_prepare_kernel(BwdArgs a, int64_t stat_groups, int chunks) {
+  __shared__ uint32_t bits[kBitsChunk];
+  if (blockIdx.x < stat_groups) {
+    row_stats<D>(a, blockIdx.x);
+  } else {
+    const int64_t i = blockIdx.x - stat_groups, column = i / chunks;
+    list_bits(a, column, (int)(i - column * chunks), bits);
+  }
 }
 
 // Order of the work.  The dense passes give each XCD (and its L2) whole heads.  The sparse
@@ -829,14 +828,13 @@ static hipError_t launch_passes(const BwdArgs& a, hipStream_t stream) {
 
 template <int D>
 static hipError_t launch_bwd(const BwdArgs& a, bool dense, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.bh * a.n_q * a.block;
   constexpr int RPW = 256 / (D / 8);
-  if (rows > 0) attn_bwd_stats_kernel<D><<<(rows + RPW - 1) / RPW, 256, 0, stream>>>(a);
+  const int64_t stat_groups = ((int64_t)a.bh * a.n_q * a.block + RPW - 1) / RPW;
+  const int chunks = (a.n_k + kBitsChunk - 1) / kBitsChunk;
+  const int64_t grid = stat_groups + (dense ? 0 : (int64_t)a.bh * a.n_words * chunks);
+  if (grid > 0) attn_bwd_prepare_kernel<D><<<grid, 256, 0, stream>>>(a, stat_groups, chunks);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (dense) return launch_passes<D, 4, true>(a, stream);
-  const dim3 grid((unsigned)((int64_t)a.bh * a.n_words), (unsigned)((a.n_k + kBitsChunk - 1) / kBitsChunk));
-  if (rows > 0) attn_bwd_bits_kernel<<<grid, 1024, 0, stream>>>(a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   return a.block == 64 ? launch_passes<D, 2, false>(a, stream) : launch_passes<D, 4, false>(a, stream);
 }
 

@@ -2,6 +2,9 @@
 // reductions, the LDS transpose read, and direct-to-LDS tile loads.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "device_common.h"
 
 namespace sparstar {
@@ -105,6 +108,16 @@ template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// f(0), .., f(N - 1) with each index a compile-time constant
+template <class F, int... I>
+__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for(f, std::make_integer_sequence<int, N>{});
 }
 
 }  // namespace sparstar

@@ -7,9 +7,6 @@
 // Two kernels.  Calls of more than 32 query rows are bound by the matrix cores and the
 // VALU (cache_attn_kernel); up to 32 rows, single tokens above all, they stream the cache
 // (cache_token_kernel).
-#include <type_traits>
-#include <utility>
-
 #include "attn_device.h"
 
 namespace sparstar {
@@ -347,16 +344,6 @@ struct CachePipe : CacheCfg<D> {
   static constexpr int P = 4, PV = 6;           // MFMAs between a K (V) operand's read and its use
   static_assert(NA == 8 && NB == 8, "a step is 16 MFMAs");
 };
-
-// f(0), .., f(N - 1) with each index a compile-time constant
-template <class F, int... I>
-__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void static_for(F&& f) {
-  static_for(f, std::make_integer_sequence<int, N>{});
-}
 
 // A raw buffer over `bytes` bytes, in scalar registers.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint8_t* p, uint32_t bytes) {

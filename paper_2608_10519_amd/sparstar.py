@@ -8,6 +8,7 @@ library cannot be loaded, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Sequence
 
@@ -348,23 +349,35 @@ def sparstar_token_topk_mass(q: torch.Tensor, k: torch.Tensor, rows: Sequence[in
     return mass
 
 
-def _like(t: torch.Tensor | None, shape, dtype, name: str) -> int | None:
-    """Pointer of an optional contiguous GPU tensor of this shape and type."""
+def _like(t: torch.Tensor | None, shape, dtype, name: str, device: torch.device) -> int | None:
+    """Pointer of an optional contiguous tensor of this shape, type and device."""
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on the GPU of shape {tuple(shape)}")
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device} of shape {tuple(shape)}")
     return t.data_ptr()
 
 
-def _lists(num: torch.Tensor, idx: torch.Tensor, B: int, H: int, Lq: int, block_size: int) -> tuple[int, int, int]:
+def _launch(fn: str, device: torch.device, *args) -> None:
+    """Calls the library on the device's current stream (and with the device current)."""
+    if device.index == torch.cuda.current_device():
+        rc = getattr(load(), fn)(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(load(), fn)(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    _check(fn, rc)
+
+
+def _lists(num: torch.Tensor, idx: torch.Tensor, B: int, H: int, Lq: int, block_size: int,
+           device: torch.device) -> tuple[int, int, int]:
     n_q = -(-Lq // block_size)
     if idx.dim() != 4:
         raise ValueError("kv_indices must be [B, H, n_q, kv_stride]")
-    return (_like(num, (B, H, n_q), torch.int32, "kv_num_blocks"),
-            _like(idx, (B, H, n_q, idx.shape[-1]), torch.int32, "kv_indices"), idx.shape[-1])
+    return (_like(num, (B, H, n_q), torch.int32, "kv_num_blocks", device),
+            _like(idx, (B, H, n_q, idx.shape[-1]), torch.int32, "kv_indices", device), idx.shape[-1])
 
 
+@functools.lru_cache(maxsize=1024)
 def sparstar_attn_bwd_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int) -> int:
     return int(load().sparstar_attn_bwd_workspace_bytes(B, H, Lq, Lk, D, block_size))
 
@@ -372,20 +385,18 @@ def sparstar_attn_bwd_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int, 
 def _attn_bwd(fn, q, k, v, o, lse, d_o, lists, block_size, softmax_scale, dlse, out, workspace):
     B, H, Lq, D = _bhld(q, "q")
     _, _, Lk, _ = _bhld(k, "k")
-    bf16 = torch.bfloat16
-    kp, vp = (_like(t, (B, H, Lk, D), bf16, n) for t, n in ((k, "k"), (v, "v")))
-    op, dop = (_like(t, (B, H, Lq, D), bf16, n) for t, n in ((o, "o"), (d_o, "d_o")))
-    lp, dlp = (_like(t, (B, H, Lq), torch.float32, n) for t, n in ((lse, "lse"), (dlse, "dlse")))
-    listed = _lists(*lists, B, H, Lq, block_size) if lists is not None else ()
+    dev, bf16, f32, rows, keys = q.device, torch.bfloat16, torch.float32, q.shape, (B, H, Lk, D)
+    kp, vp = _like(k, keys, bf16, "k", dev), _like(v, keys, bf16, "v", dev)
+    op, dop = _like(o, rows, bf16, "o", dev), _like(d_o, rows, bf16, "d_o", dev)
+    lp, dlp = _like(lse, rows[:3], f32, "lse", dev), _like(dlse, rows[:3], f32, "dlse", dev)
+    listed = _lists(*lists, B, H, Lq, block_size, dev) if lists is not None else ()
     dq, dk, dv = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)) if out is None else out
-    grads = [_like(t, s.shape, bf16, n) for t, s, n in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv"))]
+    grads = _like(dq, rows, bf16, "dq", dev), _like(dk, keys, bf16, "dk", dev), _like(dv, keys, bf16, "dv", dev)
     if workspace is None:
         need = sparstar_attn_bwd_workspace_bytes(B, H, Lq, Lk, D, block_size)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
-    rc = getattr(load(), fn)(q.data_ptr(), kp, vp, op, lp, dop, dlp, B, H, Lq, Lk, D, block_size, *listed,
-                             float(softmax_scale), *grads, workspace.data_ptr(),
-                             workspace.numel() * workspace.element_size(), _stream())
-    _check(fn, rc)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    _launch(fn, dev, q.data_ptr(), kp, vp, op, lp, dop, dlp, B, H, Lq, Lk, D, block_size, *listed,
+            float(softmax_scale), *grads, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return dq, dk, dv
 
 
@@ -425,16 +436,15 @@ class KvCache(NamedTuple):
         return cls(*codes, *scales, block_size)
 
 
-def _cache(c: KvCache, B: int, H: int, D: int) -> tuple[int, list[int]]:
+def _cache(c: KvCache, B: int, H: int, D: int, device: torch.device) -> tuple[int, tuple[int, int, int, int]]:
     """(capacity, the four pointers) of a cache that fits B, H and D."""
-    if c.k.dim() != 4:
-        raise ValueError("the cache's k must be [B, H, cap, D]")
-    cap = c.k.shape[2]
-    scale = (B, H, -(-cap // c.block_size) if c.block_size > 0 else 0)
-    return cap, [_like(c.k, (B, H, cap, D), torch.float8_e4m3fn, "cache.k"),
-                 _like(c.v, (B, H, cap, D), torch.float8_e4m3fn, "cache.v"),
-                 _like(c.k_scale, scale, torch.uint8, "cache.k_scale"),
-                 _like(c.v_scale, scale, torch.uint8, "cache.v_scale")]
+    if c.k.dim() != 4 or c.block_size < 1:
+        raise ValueError("the cache's k must be [B, H, cap, D], its block size positive")
+    cap, e4m3 = c.k.shape[2], torch.float8_e4m3fn
+    codes, scale = (B, H, cap, D), (B, H, -(-cap // c.block_size))
+    return cap, (_like(c.k, codes, e4m3, "cache.k", device), _like(c.v, codes, e4m3, "cache.v", device),
+                 _like(c.k_scale, scale, torch.uint8, "cache.k_scale", device),
+                 _like(c.v_scale, scale, torch.uint8, "cache.v_scale", device))
 
 
 def sparstar_cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, start: int = 0, *,
@@ -443,53 +453,52 @@ def sparstar_cache_write(k: torch.Tensor, v: torch.Tensor, cache: KvCache, start
     each batch element (int32 on the GPU); counts[b] limits how many of the element's
     tokens are written."""
     B, H, L, D = _bhld(k, "k")
-    vp = _like(v, k.shape, torch.bfloat16, "v")
-    cap, ptrs = _cache(cache, B, H, D)
-    sp, cp = (_like(t, (B,), torch.int32, n) for t, n in ((starts, "starts"), (counts, "counts")))
-    rc = load().sparstar_cache_write(k.data_ptr(), vp, B, H, L, D, cache.block_size, start, sp, cp, cap, *ptrs,
-                                     _stream())
-    _check("sparstar_cache_write", rc)
+    dev = k.device
+    vp = _like(v, k.shape, torch.bfloat16, "v", dev)
+    cap, ptrs = _cache(cache, B, H, D, dev)
+    sp, cp = _like(starts, (B,), torch.int32, "starts", dev), _like(counts, (B,), torch.int32, "counts", dev)
+    _launch("sparstar_cache_write", dev, k.data_ptr(), vp, B, H, L, D, cache.block_size, start, sp, cp, cap, *ptrs)
 
 
 def sparstar_cache_read(cache: KvCache, start: int, L: int, *, want=("k", "v"), out=None):
     """Rows [start, start + L) of the cache in bf16, exactly: (k, v), each [B, H, L, D], or
     None for one that `want` leaves out."""
-    B, H, _, D = cache.k.shape
-    cap, ptrs = _cache(cache, B, H, D)
+    if cache.k.dim() != 4 or not cache.k.is_cuda:
+        raise ValueError("the cache's k must be [B, H, cap, D], on the GPU")
+    (B, H, _, D), dev, bf16 = cache.k.shape, cache.k.device, torch.bfloat16
+    cap, ptrs = _cache(cache, B, H, D, dev)
+    shape = (B, H, L, D)
     if out is None:
-        out = [torch.empty((B, H, L, D), dtype=torch.bfloat16, device=cache.k.device) if n in want else None
-               for n in ("k", "v")]
-    kp, vp = (_like(t, (B, H, L, D), torch.bfloat16, n) for t, n in zip(out, ("k", "v")))
-    rc = load().sparstar_cache_read(*ptrs, B, H, start, L, cap, D, cache.block_size, kp, vp, _stream())
-    _check("sparstar_cache_read", rc)
+        out = [torch.empty(shape, dtype=bf16, device=dev) if n in want else None for n in ("k", "v")]
+    kp, vp = _like(out[0], shape, bf16, "k", dev), _like(out[1], shape, bf16, "v", dev)
+    _launch("sparstar_cache_read", dev, *ptrs, B, H, start, L, cap, D, cache.block_size, kp, vp)
     return tuple(out)
 
 
+@functools.lru_cache(maxsize=1024)
 def sparstar_cache_attn_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int) -> int:
     return int(load().sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, block_size))
 
 
 def _cache_attn(fn, q, cache, lists, Lk, softmax_scale, lens, out, lse, return_lse, split, workspace):
     B, H, Lq, D = _bhld(q, "q")
-    cap, ptrs = _cache(cache, B, H, D)
+    dev, b = q.device, cache.block_size
+    cap, ptrs = _cache(cache, B, H, D, dev)
     Lk = cap if Lk is None else Lk
-    b = cache.block_size
-    lp = _like(lens, (B,), torch.int32, "lens")
-    listed = _lists(*lists, B, H, Lq, b) if lists is not None else ()
+    lp = _like(lens, (B,), torch.int32, "lens", dev)
+    listed = _lists(*lists, B, H, Lq, b, dev) if lists is not None else ()
     o = torch.empty_like(q) if out is None else out
     if lse is None and return_lse:
-        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device)
-    op, lsep = _like(o, q.shape, torch.bfloat16, "out"), _like(lse, (B, H, Lq), torch.float32, "lse")
+        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=dev)
+    op, lsep = _like(o, q.shape, torch.bfloat16, "out", dev), _like(lse, (B, H, Lq), torch.float32, "lse", dev)
     wp, wn = None, 0
     if split:
         if workspace is None:
             need = sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, b)
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
         if workspace is not None:
             wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    rc = getattr(load(), fn)(q.data_ptr(), *ptrs, B, H, Lq, Lk, cap, D, b, lp, *listed, float(softmax_scale), op, lsep,
-                             wp, wn, _stream())
-    _check(fn, rc)
+    _launch(fn, dev, q.data_ptr(), *ptrs, B, H, Lq, Lk, cap, D, b, lp, *listed, float(softmax_scale), op, lsep, wp, wn)
     return o, lse
 
 
