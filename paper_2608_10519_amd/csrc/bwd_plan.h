@@ -3,6 +3,8 @@
 // kernels (attn_bwd.hip) take the cut through BwdArgs.
 #pragma once
 
+#include <math.h>
+
 #include <algorithm>
 
 #include "launch.h"
@@ -17,25 +19,39 @@ struct BwdPlan {
 
 constexpr int kBwdMaxRanges = 16;
 
-// Ranges of one pass: work-groups of `rows` rows that each walk `tiles` tiles, of
-// which the chip holds `held` at once.  Few work-groups leave CUs idle, so the walk
-// is cut until they fill the chip, as long as a range keeps 16 tiles.
-inline int bwd_ranges(int64_t groups, int64_t held, int64_t tiles) {
-  int r = 1;
-  while (r < kBwdMaxRanges && groups * r < 2 * held && tiles >= 32 * r) r *= 2;
-  return r;
+// Ranges of one pass: `groups` work-groups that each walk `tiles` tiles at most.  A CU works
+// off its work-groups at the rate of its matrix cores whether it holds one or two, so the
+// pass takes as long as the CU with the most of them: ceil(x) / x of the even share, x per
+// CU.  More ranges even that out (24 heads of 2,880 rows: 2.2 work-groups per CU; dQ takes
+// 3.4 ms in 2 ranges and 3.0 in 4) and cost their partial results, `bytes` written and read
+// again each, and a launch; both against a time of the pass estimated from its operations.
+inline int bwd_ranges(int64_t groups, int64_t tiles, double flops, double bytes) {
+  const double pass_us = flops / 1.1e9;
+  int best = 1;
+  double least = 0.0;
+  for (int r = 1; r <= kBwdMaxRanges && (r == 1 || tiles >= 16 * r); r *= 2) {
+    const double x = double(groups) * r / 256.0;
+    const double t = pass_us * ceil(x) / x + (r > 1 ? 4.0 + 2.0 * r * bytes / 4.5e6 : 0.0);
+    if (r == 1 || t < 0.97 * least) {
+      least = t;
+      best = r;
+    }
+  }
+  return best;
 }
 
 inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, bool dense) {
-  const int rows = dense ? 128 : block, waves = rows / 32, tile = attn_tile_keys(d);
+  const int rows = dense ? 128 : block;
   const int64_t nq = (lq + block - 1) / block, nk = (lk + block - 1) / block;
+  const int64_t q_groups = bh * ((lq + rows - 1) / rows), k_groups = bh * ((lk + rows - 1) / rows);
+  // (the workspace does not depend on the lists: a quarter of the keys is taken for them)
+  const double products = 2.0 * d * double(bh) * double(lq) * double(lk) * (dense ? 1.0 : 0.25);
   BwdPlan p{};
-  p.dq_ranges = bwd_ranges(bh * ((lq + rows - 1) / rows), 256 * 8 / waves, (lk + tile - 1) / tile);
-  const int64_t key_groups = bh * ((lk + rows - 1) / rows), held = 256 * (d == 128 ? 4 : 8) / waves;
-  p.dkv_ranges = bwd_ranges(key_groups, held, (lq + tile - 1) / tile);
+  p.dq_ranges = bwd_ranges(std::max<int64_t>(1, q_groups), (lk + 31) / 32, 3.0 * products, 4.0 * bh * lq * d);
+  p.dkv_ranges = bwd_ranges(k_groups, (lq + 31) / 32, 4.0 * products, 8.0 * bh * lk * d);
   // (the sparse walk is cut at whole words of 32 query blocks)
   if (!dense) p.dkv_ranges = (int)std::min<int64_t>(p.dkv_ranges, std::max<int64_t>(1, (nq + 31) / 32));
-  p.rounds = key_groups * p.dkv_ranges > held;
+  p.rounds = k_groups * p.dkv_ranges > 256 * (d == 128 ? 4 : 8) / (rows / 32);
   auto align = [](size_t x) { return (x + 255) & ~size_t(255); };
   p.stats = 0;
   p.bits = align(size_t(bh * nq * block) * 2 * sizeof(float));
