@@ -19,18 +19,20 @@ struct BwdPlan {
 
 constexpr int kBwdMaxRanges = 16;
 
-// Ranges of one pass: `groups` work-groups that each walk `tiles` tiles at most.  A CU works
-// off its work-groups at the rate of its matrix cores whether it holds one or two, so the
-// pass takes as long as the CU with the most of them: ceil(x) / x of the even share, x per
-// CU.  More ranges even that out (24 heads of 2,880 rows: 2.2 work-groups per CU; dQ takes
-// 3.4 ms in 2 ranges and 3.0 in 4) and cost their partial results, `bytes` written and read
-// again each, and a launch; both against a time of the pass estimated from its operations.
-inline int bwd_ranges(int64_t groups, int64_t tiles, double flops, double bytes) {
+// Ranges of one pass: `groups` work-groups of `waves` waves that each walk `tiles` tiles at
+// most.  A SIMD works off its waves at the rate of its matrix core whether it holds one or
+// two, so the pass takes as long as the SIMDs with the most of them: ceil(x) / x of the even
+// share, x waves per SIMD.  More ranges even that out (24 dense heads of 2,880 rows: 2.2
+// work-groups of 4 waves per CU; dQ takes 3.4 ms in 2 ranges and 3.0 in 4; one head of 72,000
+// rows, block 128: both gradients 2.37 ms in 1 and 1 ranges and 1.92 in 4 and 2) and cost
+// their partial results, `bytes` written and read again each, and a launch; both against a
+// time of the pass estimated from its operations.  A gain below 3 % is not worth the memory.
+inline int bwd_ranges(int64_t groups, int waves, int64_t tiles, double flops, double bytes) {
   const double pass_us = flops / 1.1e9;
   int best = 1;
   double least = 0.0;
   for (int r = 1; r <= kBwdMaxRanges && (r == 1 || tiles >= 16 * r); r *= 2) {
-    const double x = double(groups) * r / 256.0;
+    const double x = double(groups) * r * waves / 1024.0;
     const double t = pass_us * ceil(x) / x + (r > 1 ? 4.0 + 2.0 * r * bytes / 4.5e6 : 0.0);
     if (r == 1 || t < 0.97 * least) {
       least = t;
@@ -47,8 +49,10 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   // (the workspace does not depend on the lists: a quarter of the keys is taken for them)
   const double products = 2.0 * d * double(bh) * double(lq) * double(lk) * (dense ? 1.0 : 0.25);
   BwdPlan p{};
-  p.dq_ranges = bwd_ranges(std::max<int64_t>(1, q_groups), (lk + 31) / 32, 3.0 * products, 4.0 * bh * lq * d);
-  p.dkv_ranges = bwd_ranges(k_groups, (lq + 31) / 32, 4.0 * products, 8.0 * bh * lk * d);
+  p.dq_ranges = bwd_ranges(std::max<int64_t>(1, q_groups), rows / 32, (lk + 31) / 32, 3.0 * products,
+                           4.0 * bh * lq * d);
+  p.dkv_ranges = bwd_ranges(k_groups, rows / 32, (lq + 31) / 32, 4.0 * products,
+                            8.0 * bh * lk * d);
   // (the sparse walk is cut at whole words of 32 query blocks)
   if (!dense) p.dkv_ranges = (int)std::min<int64_t>(p.dkv_ranges, std::max<int64_t>(1, (nq + 31) / 32));
   p.rounds = k_groups * p.dkv_ranges > 256 * (d == 128 ? 4 : 8) / (rows / 32);
