@@ -62,10 +62,12 @@ __device__ __forceinline__ void wait_loads_and_lds() {
 }
 
 // Writes the lane's query row (its columns 32 t + 8 g + 4 h + 0..3): O and lse, or, with
-// several ranges, the range's unnormalised P V in fp16, scaled by a power of two so that
-// its largest magnitude lies in [0.5, 1), with the running max (log2 units), the two row
-// sums and the scale's exponent.  m, l and le are the row's; l == 0 means no key was seen
-// (a NaN passes on).
+// several ranges, the range's unnormalised P V in fp16 with the running max (log2 units),
+// the two row sums and the exponent of the scale.  fp16 rounds once more, by at most 2^-11
+// of the value, an eighth of what P's rounding to bf16 may change, for half the bytes of
+// fp32.  The scale, a power of two, brings the row's largest magnitude to [2^14, 2^15), the
+// top of fp16's range, so that a column down to 2^-28 of it keeps all 11 bits.  m, l and le
+// are the row's; l == 0 means no key was seen (a NaN passes on).
 template <int D>
 __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, int64_t row, int range,
                                            const f32x16 (&acc)[D / 32], float m, float l, float le, int hh) {
@@ -81,7 +83,7 @@ __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, i
   const int64_t at = bh * a.lq + row;
   if (a.ranges > 1) {
     int ex = 0;
-    if (amax > 0.f && amax <= 3.402823466e38f) ex = __builtin_amdgcn_frexp_expf(amax);
+    if (amax > 0.f && amax <= 3.402823466e38f) ex = __builtin_amdgcn_frexp_expf(amax) - 15;
     ex = ex < -126 ? -126 : ex;
     const float sc = __builtin_amdgcn_ldexpf(1.0f, -ex);
     const int64_t prow = (int64_t)range * a.bh * a.lq + at;
