@@ -248,15 +248,20 @@ struct DqCfg : BwdCfg<D, 32> {
   static constexpr bool START = D == 64;
 };
 
+template <int D>
+struct alignas(1024) DqLds {
+  uint16_t ks[DqCfg<D>::RING][DqCfg<D>::TILE], vs[DqCfg<D>::RING][DqCfg<D>::TILE];
+};
+
+// (index: of groups work-groups)
 template <int D, int NW, bool DENSE>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void attn_bwd_dq_kernel(BwdArgs a) {
+__device__ __forceinline__ void attn_bwd_dq(const BwdArgs& a, DqLds<D>& lds, uint32_t index, uint32_t groups) {
   using C = DqCfg<D>;
   constexpr int ROWS = 32 * NW, SUB = ROWS / C::KB;  // (sparse: a list entry is SUB tiles)
-  __shared__ __attribute__((aligned(1024))) uint16_t ks[C::RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t vs[C::RING][C::TILE];
+  auto& ks = lds.ks;
+  auto& vs = lds.vs;
   const int64_t n_g = (a.lq + ROWS - 1) / ROWS;
-  const int64_t w = DENSE ? xcd_linear(blockIdx.x, gridDim.x) : blockIdx.x;
+  const int64_t w = DENSE ? xcd_linear(index, groups) : index;
   const int64_t pair = w / n_g;
   const int qg = (int)(w - pair * n_g);
   const int64_t bh = pair / a.dq_ranges;
@@ -522,17 +527,22 @@ struct DkvCfg : BwdCfg<D, 32> {
   static constexpr int WAVES = D == 128 ? 1 : 2;   // per SIMD
 };
 
+template <int D>
+struct alignas(1024) DkvLds {
+  uint16_t qs[DkvCfg<D>::RING][DkvCfg<D>::TILE], dos[DkvCfg<D>::RING][DkvCfg<D>::TILE];
+  float st[DkvCfg<D>::RING][64];
+};
+
 template <int D, int NW, bool DENSE>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DkvCfg<D>::WAVES, DkvCfg<D>::WAVES)))
-void attn_bwd_dkv_kernel(BwdArgs a) {
+__device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, uint32_t index, uint32_t groups) {
   using C = DkvCfg<D>;
   constexpr int KEYS = 32 * NW, SUB = KEYS / C::KB;  // (sparse: a query block is SUB tiles)
-  __shared__ __attribute__((aligned(1024))) uint16_t qs[C::RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint16_t dos[C::RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) float st[C::RING][64];
+  auto& qs = lds.qs;
+  auto& dos = lds.dos;
+  auto& st = lds.st;
   const int64_t n_g = (a.lk + KEYS - 1) / KEYS;
   const int64_t items = (int64_t)a.bh * a.dkv_ranges * n_g;
-  const int64_t w = DENSE ? xcd_linear(blockIdx.x, gridDim.x) : blockIdx.x % items;
+  const int64_t w = DENSE ? xcd_linear(index, groups) : index % items;
   const int64_t pair = w / n_g;
   const int kg = (int)(w - pair * n_g);
   const int64_t bh = pair / a.dkv_ranges;
@@ -548,7 +558,7 @@ void attn_bwd_dkv_kernel(BwdArgs a) {
     for (int i = lane; i < a.n_words; i += 64) n += __builtin_popcount(words[i]);
 #pragma unroll
     for (int s = 32; s > 0; s /= 2) n += __shfl_xor(n, s);
-    if ((__builtin_amdgcn_readfirstlane(n) > a.long_first) != (blockIdx.x < items)) return;
+    if ((__builtin_amdgcn_readfirstlane(n) > a.long_first) != (index < items)) return;
   }
   const int64_t key = (int64_t)kg * KEYS + wave * 32 + l32;
   const bool key_ok = key < a.lk;
@@ -776,7 +786,7 @@ void attn_bwd_dkv_kernel(BwdArgs a) {
       const int64_t o = at + 32 * t + 8 * g;
       const f32x16 &x = dk[t], &y = dv[t];
       if (a.dkv_ranges > 1) {
-        float* part = a.part + (int64_t)range * 2 * all;
+        float* part = a.part_kv + (int64_t)range * 2 * all;
         *reinterpret_cast<float4*>(part + o) = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
         *reinterpret_cast<float4*>(part + all + o) = make_float4(y[4 * g], y[4 * g + 1], y[4 * g + 2], y[4 * g + 3]);
       } else {
@@ -786,6 +796,36 @@ void attn_bwd_dkv_kernel(BwdArgs a) {
             make_uint2(pack2_bf16(y[4 * g], y[4 * g + 1]), pack2_bf16(y[4 * g + 2], y[4 * g + 3]));
       }
     }
+}
+
+template <int D, int NW, bool DENSE>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void attn_bwd_dq_kernel(BwdArgs a) {
+  __shared__ DqLds<D> lds;
+  attn_bwd_dq<D, NW, DENSE>(a, lds, blockIdx.x, gridDim.x);
+}
+
+template <int D, int NW, bool DENSE>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DkvCfg<D>::WAVES, DkvCfg<D>::WAVES)))
+void attn_bwd_dkv_kernel(BwdArgs a) {
+  __shared__ DkvLds<D> lds;
+  attn_bwd_dkv<D, NW, DENSE>(a, lds, blockIdx.x, gridDim.x);
+}
+
+// Both passes in one launch, for calls of up to two waves per SIMD: neither waits for the
+// other's last work-group.  At D = 128 dQ gives up its second wave per SIMD for it, so calls
+// of many rounds keep their launches.  Two heads of 512 x 1,152, D = 64: 16.9 us, in two
+// launches 25.5; 4 heads of 1,024 x 3,000 at 25%: 37.3 and 47.7; 8 heads: 53.4 and 59.2.
+constexpr int kBothWaves = 2048;
+template <int D, int NW, bool DENSE>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DkvCfg<D>::WAVES, DkvCfg<D>::WAVES)))
+void attn_bwd_both_kernel(BwdArgs a, uint32_t dq_groups) {
+  __shared__ union {
+    DqLds<D> dq;
+    DkvLds<D> dkv;
+  } lds;
+  if (blockIdx.x < dq_groups) attn_bwd_dq<D, NW, DENSE>(a, lds.dq, blockIdx.x, dq_groups);
+  else attn_bwd_dkv<D, NW, DENSE>(a, lds.dkv, blockIdx.x - dq_groups, gridDim.x - dq_groups);
 }
 
 // ---- sums the ranges' partial results, in order: out = bf16(scale * sum_r part[r])
@@ -813,15 +853,20 @@ static hipError_t launch_passes(const BwdArgs& a, hipStream_t stream) {
     attn_bwd_sum_kernel<<<(n / 8 + 255) / 256, 256, 0, stream>>>(part, stride, ranges, n, scale, out);
   };
   const int64_t dq_grid = (int64_t)a.bh * a.dq_ranges * ((a.lq + ROWS - 1) / ROWS);
-  if (dq_grid > 0) attn_bwd_dq_kernel<D, NW, DENSE><<<dq_grid, 64 * NW, 0, stream>>>(a);
+  const int64_t dkv_grid = (int64_t)a.bh * a.dkv_ranges * ((a.lk + ROWS - 1) / ROWS);
+  // (with long_first the key groups take two turns, of a launch of their own)
+  if (a.long_first == 0 && (dq_grid + dkv_grid) * NW <= kBothWaves) {
+    attn_bwd_both_kernel<D, NW, DENSE><<<dq_grid + dkv_grid, 64 * NW, 0, stream>>>(a, (uint32_t)dq_grid);
+  } else {
+    if (dq_grid > 0) attn_bwd_dq_kernel<D, NW, DENSE><<<dq_grid, 64 * NW, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    attn_bwd_dkv_kernel<D, NW, DENSE><<<dkv_grid * (!DENSE && a.long_first > 0 ? 2 : 1), 64 * NW, 0, stream>>>(a);
+  }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.dq_ranges > 1) sum(a.part, nq, a.dq_ranges, nq, a.scale, a.dq);
-  const int64_t dkv_grid = (int64_t)a.bh * a.dkv_ranges * ((a.lk + ROWS - 1) / ROWS);
-  attn_bwd_dkv_kernel<D, NW, DENSE><<<dkv_grid * (!DENSE && a.long_first > 0 ? 2 : 1), 64 * NW, 0, stream>>>(a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.dkv_ranges > 1) {
-    sum(a.part, 2 * nk, a.dkv_ranges, nk, a.scale, a.dk);
-    sum(a.part + nk, 2 * nk, a.dkv_ranges, nk, 1.f, a.dv);
+    sum(a.part_kv, 2 * nk, a.dkv_ranges, nk, a.scale, a.dk);
+    sum(a.part_kv + nk, 2 * nk, a.dkv_ranges, nk, 1.f, a.dv);
   }
   return hipGetLastError();
 }

@@ -83,6 +83,7 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
   a.stats = reinterpret_cast<float*>(ws + plan.stats);
   a.bits = reinterpret_cast<uint32_t*>(ws + plan.bits);
   a.part = reinterpret_cast<float*>(ws + plan.part);
+  a.part_kv = reinterpret_cast<float*>(ws + plan.part_kv);
   a.dq_ranges = plan.dq_ranges;
   a.dkv_ranges = plan.dkv_ranges;
   // (twice the lists' entries per key block, if every row fills its stride)

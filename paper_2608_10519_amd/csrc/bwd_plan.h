@@ -14,7 +14,7 @@ namespace sparstar {
 struct BwdPlan {
   int dq_ranges, dkv_ranges;
   bool rounds;  // the dK/dV pass has more work-groups than the chip holds
-  size_t stats, bits, part, total;  // byte offsets of the workspace's regions, and its size
+  size_t stats, bits, part, part_kv, total;  // byte offsets of the workspace's regions, and its size
 };
 
 constexpr int kBwdMaxRanges = 16;
@@ -62,7 +62,8 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   p.part = p.bits + (dense ? 0 : align(size_t(bh * nk * ((nq + 31) / 32)) * sizeof(uint32_t)));
   const size_t dq = p.dq_ranges > 1 ? size_t(bh * lq * d) * p.dq_ranges * sizeof(float) : 0;
   const size_t dkv = p.dkv_ranges > 1 ? 2 * size_t(bh * lk * d) * p.dkv_ranges * sizeof(float) : 0;
-  p.total = p.part + std::max(dq, dkv);
+  p.part_kv = p.part + align(dq);
+  p.total = p.part_kv + dkv;
   return p;
 }
 

@@ -158,7 +158,7 @@ struct BwdArgs {
   float* stats;                  // [BH, n_q * block / 32, 2, 32]: -lse / s, -delta
   uint32_t* bits;                // [BH, n_k, n_words]: which query blocks list each key block (sparse only)
   int n_words;                   // ceil(n_q / 32)
-  float* part;                   // fp32 partial results of the ranges: dQ, then dK and dV in the same place
+  float *part, *part_kv;         // fp32 partial results of the ranges: dQ; dK and dV
   int dq_ranges, dkv_ranges;     // ranges of each list's keys, and of the queries; 1: results go out at once
   int long_first;                // key blocks on more lists than this go first (sparse only; 0: in order)
 };

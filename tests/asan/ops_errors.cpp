@@ -70,7 +70,9 @@ hipError_t launch_attn_bwd(const BwdArgs& a, int d, bool dense, hipStream_t) {
   if (!dense) CHECK((char*)a.stats + size_t(double(a.bh) * a.n_q * a.block * 8) <= (char*)a.bits);
   CHECK(a.dq_ranges >= 1 && a.dkv_ranges >= 1);
   if (a.dq_ranges > 1) CHECK(inside(a.part, 4.0 * a.bh * lq * d * a.dq_ranges));
-  if (a.dkv_ranges > 1) CHECK(inside(a.part, 8.0 * a.bh * lk * d * a.dkv_ranges));
+  if (a.dkv_ranges > 1) CHECK(inside(a.part_kv, 8.0 * a.bh * lk * d * a.dkv_ranges));
+  // (the two may be in use at the same time)
+  if (a.dq_ranges > 1) CHECK((char*)a.part + size_t(4.0 * a.bh * lq * d * a.dq_ranges) <= (char*)a.part_kv);
   CHECK(isfinite(a.scale) && isfinite(a.inv_scale) && isfinite(a.scale_log2));
   return hipErrorInvalidValue;
 }

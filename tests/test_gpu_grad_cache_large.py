@@ -37,6 +37,11 @@ GRADS = [
     (128, 128, 2, 3, 3001, 4097, 0.3, 1),
     (64, 64, 2, 3, 1999, 3001, 0.3, 1),
     (128, 64, 2, 5, 1500, 4001, None, 0),
+    # (each pass in a launch of its own)
+    (128, 128, 2, 6, 1500, 6001, 0.3, 1),
+    (64, 64, 2, 12, 1000, 4001, 0.3, 1),
+    (128, 64, 2, 8, 1500, 6001, None, 0),
+    (64, 64, 2, 8, 1500, 6001, None, 0),
 ]
 
 
