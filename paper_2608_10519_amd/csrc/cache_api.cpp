@@ -87,18 +87,23 @@ extern "C" int sparstar_cache_read(const void* k_cache, const void* v_cache, con
 
 extern "C" size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size) {
   if (check_attn_sizes(B, H, Lq, Lk, D, block_size) != SPARSTAR_OK) return 0;
-  const int64_t bh = int64_t(B) * H, nk = (Lk + block_size - 1) / block_size;
-  // (a list's length is not known here)
-  const int ranges = Lq > 32 ? (nk >= kSplits ? kSplits : 1)
-                             : cache_attn_plan(bh, Lq, Lk, D, block_size, 0, true, true).ranges;
-  return cache_attn_workspace(bh * Lq, D, ranges);
+  return cache_attn_workspace(int64_t(B) * H * Lq, D, cache_attn_most_ranges(int64_t(B) * H, Lq, Lk, block_size));
 }
 
 extern "C" void sparstar_internal_cache_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                              int64_t kv_stride, int64_t* out) {
   const CachePlan p = cache_attn_plan(int64_t(B) * H, Lq, Lk, D, block_size, kv_stride, kv_stride == 0, true);
   out[0] = p.waves;
-  out[1] = p.ranges;
+  // parts of a list that are joined: ranges, and the waves' shares of them
+  const int64_t nk = (Lk + block_size - 1) / block_size, entries = kv_stride == 0 ? nk : std::min(nk, kv_stride);
+  out[1] = p.waves == 1 ? std::min<int64_t>(entries, int64_t(p.ranges) * kTokenWaves) : p.ranges;
+}
+
+// Ranges of such a call with a workspace; kv_stride 0: dense.  1: it would not use one.
+extern "C" int sparstar_internal_cache_ranges(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                              int64_t kv_stride) {
+  if (check_attn_sizes(B, H, Lq, Lk, D, block_size) != SPARSTAR_OK) return 1;
+  return cache_attn_plan(int64_t(B) * H, Lq, Lk, D, block_size, kv_stride, kv_stride == 0, true).ranges;
 }
 
 static int cache_attn_common(const void* q, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
@@ -126,7 +131,8 @@ static int cache_attn_common(const void* q, const void* k_cache, const void* v_c
       cache_attn_plan(bh, Lq, Lk, D, block_size, dense ? 0 : kv_stride, dense, workspace != nullptr);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
     return report_error(SPARSTAR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (workspace && workspace_bytes < cache_attn_workspace(bh * Lq, D, plan.ranges))
+  if (workspace &&
+      workspace_bytes < cache_attn_workspace(bh * Lq, D, cache_attn_most_ranges(bh, Lq, Lk, block_size)))
     return report_error(SPARSTAR_ERR_WORKSPACE, "workspace is smaller than sparstar_cache_attn_workspace_bytes");
   if (Lq == 0) return clear_error();
   const double sc = softmax_scale > 0.f ? double(softmax_scale) : 1.0 / sqrt(double(D));

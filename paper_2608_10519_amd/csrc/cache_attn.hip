@@ -112,23 +112,30 @@ __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, i
   if (a.lse != nullptr && hh == 0) a.lse[at] = le == 0.f ? -INFINITY : (m + log2f(le)) * 0.69314718055994530942f;
 }
 
-// ---- up to 32 query rows: one wave per (head, range of the list), with a ring of tiles of
-// its own and no barrier.  S^T = K Q^T and O^T += V^T P^T as in attn_fwd.hip, with the
-// operands turned into bf16 in registers; mostly empty products, but the matrix cores
+// ---- up to 32 query rows: one work-group of four waves per (head, range of the list); each
+// wave has a share of the range, a ring of tiles of its own and no barrier until the four
+// join what they found through LDS.  S^T = K Q^T and O^T += V^T P^T as in attn_fwd.hip, with
+// the operands turned into bf16 in registers; mostly empty products, but the matrix cores
 // could take 34 TB/s of codes this way.  A lone wave needs 0.7 us per tile, so what counts
-// is how many there are: two tiles of K and V in LDS (16 KB) let ten run on a CU, and the
-// call cuts its lists into about 1,024 ranges, four to a CU.  24 heads of 144,512 rows: 160
-// us with two tiles, 177 with three or four; 5.5 TB/s, of some 6.2 that reading reaches.
+// is how many there are: the call cuts its lists for four waves per CU.  24 heads of 144,512
+// rows: 160 us, 5.6 TB/s of some 6.2 that reading reaches, with two tiles in LDS per wave (177
+// with three or four); one head 24.5 us, and 30.2 with every wave's result joined through
+// memory; 8 heads of 1,152 rows, D = 64, 10.7 us in one launch.
 template <int D, bool DENSE>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(3, 3)))
+__global__ __launch_bounds__(64 * kTokenWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void cache_token_kernel(CacheAttnArgs a) {
   using C = CacheCfg<D>;
-  constexpr int RING = 2;
-  __shared__ __attribute__((aligned(1024))) uint8_t ks[RING][C::TILE];
-  __shared__ __attribute__((aligned(1024))) uint8_t vs[RING][C::TILE];
+  constexpr int RING = 2, W = kTokenWaves;
+  // a wave's K and V tiles, and then what it adds to the row's sums
+  static_assert(2 * RING * C::TILE >= C::DT * 16 * 64 * 4, "a wave's sums fit its tiles");
+  __shared__ __attribute__((aligned(1024))) uint8_t tiles[W][2][RING][C::TILE];
+  __shared__ float meta[W][3][64];
   const int64_t bh = blockIdx.x / a.ranges;
   const int range = (int)(blockIdx.x - bh * a.ranges);
-  const int lane = threadIdx.x, l32 = lane % 32, hh = lane / 32;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int l32 = lane % 32, hh = lane / 32;
+  auto& ks = tiles[wave][0];
+  auto& vs = tiles[wave][1];
 
   // tokens that exist: rows past them are neither read nor attended to
   int64_t len = a.lk;
@@ -161,8 +168,9 @@ void cache_token_kernel(CacheAttnArgs a) {
       n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
       list = a.kv_indices + r * a.stride;
     }
-    first = __builtin_amdgcn_readfirstlane((int)((int64_t)n * range / a.ranges));
-    cnt = __builtin_amdgcn_readfirstlane((int)((int64_t)n * (range + 1) / a.ranges)) - first;
+    const int part = range * W + wave, parts = a.ranges * W;
+    first = __builtin_amdgcn_readfirstlane((int)((int64_t)n * part / parts));
+    cnt = __builtin_amdgcn_readfirstlane((int)((int64_t)n * (part + 1) / parts)) - first;
   }
   // Entries 64 at a time in VGPRs: the block and its scale bytes.  One that names no
   // block gives -1, whose tiles are loaded as zeros and masked.
@@ -242,7 +250,7 @@ void cache_token_kernel(CacheAttnArgs a) {
     for (int j = 0; j < ntiles; ++j) {
       const Tile nt = fetch(j + RING - 1);
       wait_loads_and_lds<2 * 4 * (RING - 2)>();  // tile j, with the tiles issued after it outstanding
-      __syncthreads();
+      asm volatile("" ::: "memory");
       issue(nt.t, slot == 0 ? RING - 1 : slot - 1);
       cur = ahead[0];
 #pragma unroll
@@ -311,9 +319,52 @@ void cache_token_kernel(CacheAttnArgs a) {
       slot = slot + 1 == RING ? 0 : slot + 1;
     }
     wait_vmcnt<0>();  // loads past the end of the list still write LDS
+    asm volatile("" ::: "memory");
   }
 
-  store_rows<D>(a, bh, row, range, acc, m_run, half_swap_sum(l_run), half_swap_sum(le_run), hh);
+  // The first wave joins the four: with M = max_w m_w, sums of 2^(m_w - M) times each one's.
+  float l = half_swap_sum(l_run), le = half_swap_sum(le_run);
+  if (wave != 0) {
+    float4* mine = reinterpret_cast<float4*>(&tiles[wave][0][0][0]) + lane;
+#pragma unroll
+    for (int i = 0; i < C::DT * 4; ++i) {
+      const f32x16& x = acc[i / 4];
+      mine[64 * i] = make_float4(x[4 * (i % 4)], x[4 * (i % 4) + 1], x[4 * (i % 4) + 2], x[4 * (i % 4) + 3]);
+    }
+    meta[wave][0][lane] = m_run;
+    meta[wave][1][lane] = l;
+    meta[wave][2][lane] = le;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  float m = m_run;
+#pragma unroll
+  for (int w = 1; w < W; ++w) m = fmaxf(m, meta[w][0][lane]);
+  // (a wave that saw no key has m = -inf and sums of zero, a NaN among its sums passes on)
+  auto weight = [&](float x) { return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - m); };
+  const float own = weight(m_run);
+  l *= own;
+  le *= own;
+#pragma unroll
+  for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[t][e] *= own;
+#pragma unroll
+  for (int w = 1; w < W; ++w) {
+    const float f = weight(meta[w][0][lane]);
+    l = fmaf(meta[w][1][lane], f, l);
+    le = fmaf(meta[w][2][lane], f, le);
+    const float4* theirs = reinterpret_cast<const float4*>(&tiles[w][0][0][0]) + lane;
+#pragma unroll
+    for (int i = 0; i < C::DT * 4; ++i) {
+      const float4 u = theirs[64 * i];
+      f32x16& x = acc[i / 4];
+      const int e = 4 * (i % 4);
+      x[e] = fmaf(u.x, f, x[e]), x[e + 1] = fmaf(u.y, f, x[e + 1]);
+      x[e + 2] = fmaf(u.z, f, x[e + 2]), x[e + 3] = fmaf(u.w, f, x[e + 3]);
+    }
+  }
+  store_rows<D>(a, bh, row, range, acc, m, l, le, hh);
 }
 
 // ---- more than 32 query rows: one work-group per (head, range of the list, 32 NW rows),
@@ -812,7 +863,7 @@ static hipError_t launch_merge(const CacheAttnArgs& a, hipStream_t stream) {
 template <int D, bool DENSE>
 static hipError_t launch_mode(const CacheAttnArgs& a, int waves, hipStream_t stream) {
   if (waves == 1) {
-    cache_token_kernel<D, DENSE><<<(int64_t)a.bh * a.ranges, 64, 0, stream>>>(a);
+    cache_token_kernel<D, DENSE><<<(int64_t)a.bh * a.ranges, 64 * kTokenWaves, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return launch_merge<D, 16>(a, stream);
   }

@@ -17,21 +17,31 @@ struct CachePlan {
   int64_t grid;
 };
 
-constexpr int kCacheMaxTokenRanges = 256;
+constexpr int kCacheMaxTokenRanges = 64;
+
+// The most ranges that a call of these sizes is cut into, whatever its lists hold.
+inline int cache_attn_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block) {
+  const int64_t nk = (lk + block - 1) / block;
+  if (lq > 32) return nk >= kSplits ? kSplits : 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / kTokenWaves / bh, nk, kCacheMaxTokenRanges}));
+}
 
 // kv_stride: entries that a list can hold; ignored for the dense call.
 inline CachePlan cache_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
                                  bool may_split) {
   const int64_t nk = (lk + block - 1) / block;
   if (lq <= 32) {
-    // A few rows stream the cache: single waves, four to a CU (with more, some CUs get five or
-    // six and the call waits for them: 1,792 waves 166 us, 2,560 197, 1,024 172 for two
-    // sequences of 24 heads, 84,032 and 67,226 rows; of 24 heads, 8,000 rows, 24, 24 and 18).
-    // A wave reads two blocks at least, and a row's ranges are bounded, since joining them
-    // costs as much as reading them (one head of 144,512 rows: 256 ranges 31 us, 1,024 49).
-    const int64_t want = 1024 / bh, entries = dense ? nk : std::min(nk, kv_stride);
+    // A few rows stream the cache: four waves to a CU (with more, some CUs get five or six and
+    // the call waits for them: 1,792 waves 166 us, 2,560 197, 1,024 172 for two sequences of
+    // 24 heads, 84,032 and 67,226 rows).  A second launch that joins ranges costs what 12 tiles
+    // of a wave cost (8 heads, D = 128: 1,024 rows in one range 11.1 us, in two 15.0; 2,048 rows
+    // 17.5 and 14.9).  A wave reads four tiles at least, and a row's ranges are bounded, since
+    // joining them costs as much as reading them.
+    const int64_t entries = dense ? nk : std::min(nk, kv_stride), tiles = entries * (block / attn_tile_keys(d));
+    const int64_t most = cache_attn_most_ranges(bh, lq, lk, block);
     CachePlan p{1, 1, 0, 0, 0};
-    if (may_split) p.ranges = (int)std::max<int64_t>(1, std::min<int64_t>({want, entries / 2, kCacheMaxTokenRanges}));
+    if (may_split && tiles >= 12 * kTokenWaves)
+      p.ranges = (int)std::min<int64_t>(most, tiles / (4 * kTokenWaves));
     p.grid = bh * p.ranges;
     return p;
   }

@@ -185,6 +185,9 @@ struct CacheReadArgs {
   int bh, d, block;
 };
 
+// Waves of a work-group of the kernel for up to 32 query rows, each with a share of the keys.
+constexpr int kTokenWaves = 4;
+
 struct CacheAttnArgs {
   const uint16_t* q;               // [BH, Lq, D] bf16
   const uint8_t *k_cache, *v_cache, *k_scale, *v_scale;

@@ -91,6 +91,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.sparstar_cache_read.restype = c_i
     lib.sparstar_cache_attn_workspace_bytes.argtypes = [c_i, c_i, c_i64, c_i64, c_i, c_i]
     lib.sparstar_cache_attn_workspace_bytes.restype = c_sz
+    lib.sparstar_internal_cache_ranges.argtypes = [c_i, c_i, c_i64, c_i64, c_i, c_i, c_i64]
+    lib.sparstar_internal_cache_ranges.restype = c_i
     lib.sparstar_cache_sparse_attn_fwd.argtypes = [c_p] * 5 + [c_i, c_i, c_i64, c_i64, c_i64, c_i, c_i, c_p, c_p, c_p,
                                                                c_i, c_f, c_p, c_p, c_p, c_sz, c_p]
     lib.sparstar_cache_sparse_attn_fwd.restype = c_i
@@ -480,6 +482,14 @@ def sparstar_cache_attn_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int
     return int(load().sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, block_size))
 
 
+@functools.lru_cache(maxsize=1024)
+def _cache_scratch(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int, kv_stride: int) -> int:
+    """Bytes of workspace that a call makes use of (kv_stride 0: the dense one)."""
+    if load().sparstar_internal_cache_ranges(B, H, Lq, Lk, D, block_size, kv_stride) <= 1:
+        return 0
+    return sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, block_size)
+
+
 def _cache_attn(fn, q, cache, lists, Lk, softmax_scale, lens, out, lse, return_lse, split, workspace):
     B, H, Lq, D = _bhld(q, "q")
     dev, b = q.device, cache.block_size
@@ -494,7 +504,7 @@ def _cache_attn(fn, q, cache, lists, Lk, softmax_scale, lens, out, lse, return_l
     wp, wn = None, 0
     if split:
         if workspace is None:
-            need = sparstar_cache_attn_workspace_bytes(B, H, Lq, Lk, D, b)
+            need = _cache_scratch(B, H, Lq, Lk, D, b, listed[2] if listed else 0)
             workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
         if workspace is not None:
             wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
