@@ -215,10 +215,29 @@ __device__ __forceinline__ void list_bits(const BwdArgs& a, int64_t column, int 
   for (int j = threadIdx.x; j < hi - lo; j += 256) a.bits[(bh * a.n_k + lo + j) * a.n_words + word] = bits[j];
 }
 
-// Both in one launch: the first `stat_groups` work-groups take the rows.
+// ---- the key blocks that are taken first: 8 threads count a block's bits.  Where a block's
+// pieces stand in the list differs from call to call, what is computed for them does not.
+__global__ __launch_bounds__(256) void attn_bwd_pieces_kernel(BwdArgs a) {
+  const int64_t n = (int64_t)a.bh * a.n_k, i = (int64_t)blockIdx.x * 32 + threadIdx.x / 8;
+  int count = 0;
+  if (i < n)
+    for (int w = threadIdx.x % 8; w < a.n_words; w += 8) count += __builtin_popcount(a.bits[i * a.n_words + w]);
+#pragma unroll
+  for (int s = 4; s > 0; s /= 2) count += __shfl_xor(count, s, 8);
+  if (i >= n || threadIdx.x % 8 != 0) return;
+  a.listed[i] = count > a.list_min;
+  if (count <= a.list_min) return;
+  const int pieces = (count + a.piece_max - 1) / a.piece_max;
+  const int at = atomicAdd(a.piece_count, pieces);
+  const int slot = pieces > 1 ? atomicAdd(a.piece_count + 1, pieces) : 0;
+  for (int p = 0; p < pieces; ++p) a.pieces[at + p] = make_int4((int)i, p, pieces, slot);
+}
+
+// Statistics and bits in one launch: the first `stat_groups` work-groups take the rows.
 template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_prepare_kernel(BwdArgs a, int64_t stat_groups, int chunks) {
   __shared__ uint32_t bits[kBitsChunk];
+  if (a.list_min > 0 && blockIdx.x == 0 && threadIdx.x < 2) a.piece_count[threadIdx.x] = 0;
   if (blockIdx.x < stat_groups) {
     row_stats<D>(a, blockIdx.x);
   } else {
@@ -541,25 +560,36 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
   auto& dos = lds.dos;
   auto& st = lds.st;
   const int64_t n_g = (a.lk + KEYS - 1) / KEYS;
-  const int64_t items = (int64_t)a.bh * a.dkv_ranges * n_g;
-  const int64_t w = DENSE ? xcd_linear(index, groups) : index % items;
-  const int64_t pair = w / n_g;
-  const int kg = (int)(w - pair * n_g);
-  const int64_t bh = pair / a.dkv_ranges;
-  const int range = (int)(pair - bh * a.dkv_ranges);
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int l32 = lane % 32, hh = lane / 32;
-
   // Key blocks that far more queries list than the average (forced ones: all of them) come
-  // first, in a turn of their own through the items: begun last they would run on alone.
-  if (!DENSE && a.long_first > 0) {
-    const uint32_t* words = a.bits + (bh * a.n_k + kg) * a.n_words;
-    int n = 0;
-    for (int i = lane; i < a.n_words; i += 64) n += __builtin_popcount(words[i]);
-#pragma unroll
-    for (int s = 32; s > 0; s /= 2) n += __shfl_xor(n, s);
-    if ((__builtin_amdgcn_readfirstlane(n) > a.long_first) != (index < items)) return;
+  // first: begun last they would run on alone.
+  // (The grid holds the pieces, as many as there can be, and every block; a block among the
+  // pieces returns here, and so do work-groups past the end.)
+  int slot = -1, range = 0, ranges = a.dkv_ranges, kg;
+  int64_t bh;
+  if (!DENSE && a.list_min > 0) {
+    const int first = __builtin_amdgcn_readfirstlane(*a.piece_count);
+    int item = (int)index - first;
+    if (item < 0) {
+      const int4 p = a.pieces[index];
+      item = __builtin_amdgcn_readfirstlane(p.x);
+      range = __builtin_amdgcn_readfirstlane(p.y);
+      ranges = __builtin_amdgcn_readfirstlane(p.z);
+      slot = __builtin_amdgcn_readfirstlane(p.w) + range;
+    } else if (item >= a.bh * (int)n_g || __builtin_amdgcn_readfirstlane((int)a.listed[item]) != 0) {
+      return;
+    }
+    bh = item / (int)n_g;
+    kg = item - (int)bh * (int)n_g;
+  } else {
+    const int64_t w = DENSE ? xcd_linear(index, groups) : index;
+    const int64_t pair = w / n_g;
+    kg = (int)(w - pair * n_g);
+    bh = pair / ranges;
+    range = (int)(pair - bh * ranges);
   }
+
   const int64_t key = (int64_t)kg * KEYS + wave * 32 + l32;
   const bool key_ok = key < a.lk;
   bf16x8 kf[C::DS], vf[C::DS];
@@ -576,17 +606,20 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
   // block's words, 64 words at a time in a VGPR.
   const uint32_t* words = nullptr;
   int wpos, wend;            // words (dense: tiles) still to load, end of the range
+  int b0 = 0, b1 = 0;        // the range's query blocks
   uint32_t wreg = 0, cur = 0;
   uint64_t full = 0;         // words of the batch that have bits left
   int wbase = 0, qb32 = 0, sub = SUB, blk = 0;
   if constexpr (DENSE) {
     const int64_t n = (a.lq + C::KB - 1) / C::KB;
-    wpos = (int)(n * range / a.dkv_ranges);
-    wend = (int)(n * (range + 1) / a.dkv_ranges);
+    wpos = (int)(n * range / ranges);
+    wend = (int)(n * (range + 1) / ranges);
   } else {
     words = a.bits + (bh * a.n_k + kg) * a.n_words;
-    wpos = (int)((int64_t)a.n_words * range / a.dkv_ranges);
-    wend = (int)((int64_t)a.n_words * (range + 1) / a.dkv_ranges);
+    b0 = (int)((int64_t)a.n_q * range / ranges);
+    b1 = (int)((int64_t)a.n_q * (range + 1) / ranges);
+    wpos = b0 / 32;
+    wend = (b1 + 31) / 32;
   }
   auto next_tile = [&]() -> int {  // -1: none is left
     if constexpr (DENSE) {
@@ -598,6 +631,9 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
             if (wpos >= wend) return -1;
             wbase = wpos;
             wreg = wpos + lane < wend ? words[wpos + lane] : 0u;
+            const int first = (wpos + lane) * 32, last = first + 32;
+            if (first < b0) wreg &= ~0u << (b0 - first);
+            if (last > b1 && wreg != 0) wreg &= ~0u >> (last - b1);
             full = __builtin_amdgcn_ballot_w64(wreg != 0);
             wpos += 64;
           }
@@ -778,21 +814,25 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
     wait_vmcnt<0>();  // loads past the end of the walk still write LDS
   }
   if (!key_ok) return;
-  const int64_t at = (bh * a.lk + key) * D + 4 * hh, all = (int64_t)a.bh * a.lk * D;
+  const int64_t at = (bh * a.lk + key) * D + 4 * hh;
+  // partial results: of whole tensors, or of a piece
+  const int64_t all = slot < 0 ? (int64_t)a.bh * a.lk * D : (int64_t)KEYS * D;
+  float* const part = slot < 0 ? a.part_kv + range * 2 * all + at
+                               : a.part_piece + slot * 2 * all + (wave * 32 + l32) * D + 4 * hh;
 #pragma unroll
   for (int t = 0; t < C::DT; ++t)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int64_t o = at + 32 * t + 8 * g;
+      const int64_t o = 32 * t + 8 * g;
       const f32x16 &x = dk[t], &y = dv[t];
-      if (a.dkv_ranges > 1) {
-        float* part = a.part_kv + (int64_t)range * 2 * all;
+      if (ranges > 1) {
         *reinterpret_cast<float4*>(part + o) = make_float4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
         *reinterpret_cast<float4*>(part + all + o) = make_float4(y[4 * g], y[4 * g + 1], y[4 * g + 2], y[4 * g + 3]);
       } else {
-        *reinterpret_cast<uint2*>(a.dk + o) = make_uint2(pack2_bf16(x[4 * g] * a.scale, x[4 * g + 1] * a.scale),
-                                                         pack2_bf16(x[4 * g + 2] * a.scale, x[4 * g + 3] * a.scale));
-        *reinterpret_cast<uint2*>(a.dv + o) =
+        *reinterpret_cast<uint2*>(a.dk + at + o) =
+            make_uint2(pack2_bf16(x[4 * g] * a.scale, x[4 * g + 1] * a.scale),
+                       pack2_bf16(x[4 * g + 2] * a.scale, x[4 * g + 3] * a.scale));
+        *reinterpret_cast<uint2*>(a.dv + at + o) =
             make_uint2(pack2_bf16(y[4 * g], y[4 * g + 1]), pack2_bf16(y[4 * g + 2], y[4 * g + 3]));
       }
     }
@@ -845,6 +885,34 @@ __global__ __launch_bounds__(256) void attn_bwd_sum_kernel(const float* part, in
                  pack2_bf16(y.x * scale, y.y * scale), pack2_bf16(y.z * scale, y.w * scale));
 }
 
+// ---- the same for key blocks that were cut, an eighth of a block's dK and dV at a time
+constexpr int kPieceSumGroups = 2048;
+template <int D>
+__global__ __launch_bounds__(256) void attn_bwd_piece_sum_kernel(BwdArgs a) {
+  const int n = *a.piece_count, all = a.block * D;
+  for (int w = blockIdx.x; w < 8 * n; w += kPieceSumGroups) {
+    const int4 p = a.pieces[w / 8];
+    if (p.y != 0 || p.z <= 1) continue;  // (a block's first piece stands for it)
+    const int64_t bh = p.x / a.n_k, kg = p.x - bh * a.n_k, left = a.lk - kg * a.block;
+    const float* part = a.part_piece + (int64_t)p.w * 2 * all;
+    const int valid = (int)(left < a.block ? left : a.block) * D;
+    for (int i = (w % 8 * 256 + threadIdx.x) * 4; i < 2 * all; i += 8 * 256 * 4) {
+      const bool is_v = i >= all;
+      const int at = is_v ? i - all : i;
+      if (at >= valid) continue;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int r = 0; r < p.z; ++r) {
+        const float4 u = *reinterpret_cast<const float4*>(part + (int64_t)r * 2 * all + i);
+        x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w;
+      }
+      const float s = is_v ? 1.f : a.scale;
+      uint16_t* out = (is_v ? a.dv : a.dk) + (bh * a.lk + kg * a.block) * D + at;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack2_bf16(x.x * s, x.y * s), pack2_bf16(x.z * s, x.w * s));
+    }
+  }
+}
+
 template <int D, int NW, bool DENSE>
 static hipError_t launch_passes(const BwdArgs& a, hipStream_t stream) {
   constexpr int ROWS = 32 * NW;
@@ -854,16 +922,16 @@ static hipError_t launch_passes(const BwdArgs& a, hipStream_t stream) {
   };
   const int64_t dq_grid = (int64_t)a.bh * a.dq_ranges * ((a.lq + ROWS - 1) / ROWS);
   const int64_t dkv_grid = (int64_t)a.bh * a.dkv_ranges * ((a.lk + ROWS - 1) / ROWS);
-  // (with long_first the key groups take two turns, of a launch of their own)
-  if (a.long_first == 0 && (dq_grid + dkv_grid) * NW <= kBothWaves) {
-    attn_bwd_both_kernel<D, NW, DENSE><<<dq_grid + dkv_grid, 64 * NW, 0, stream>>>(a, (uint32_t)dq_grid);
+  if ((dq_grid + dkv_grid) * NW <= kBothWaves) {
+    attn_bwd_both_kernel<D, NW, DENSE><<<dq_grid + dkv_grid + a.most_pieces, 64 * NW, 0, stream>>>(a, (uint32_t)dq_grid);
   } else {
     if (dq_grid > 0) attn_bwd_dq_kernel<D, NW, DENSE><<<dq_grid, 64 * NW, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    attn_bwd_dkv_kernel<D, NW, DENSE><<<dkv_grid * (!DENSE && a.long_first > 0 ? 2 : 1), 64 * NW, 0, stream>>>(a);
+    attn_bwd_dkv_kernel<D, NW, DENSE><<<dkv_grid + a.most_pieces, 64 * NW, 0, stream>>>(a);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (a.dq_ranges > 1) sum(a.part, nq, a.dq_ranges, nq, a.scale, a.dq);
+  if (a.list_min > 0 && a.piece_max < a.n_q) attn_bwd_piece_sum_kernel<D><<<kPieceSumGroups, 256, 0, stream>>>(a);
   if (a.dkv_ranges > 1) {
     sum(a.part_kv, 2 * nk, a.dkv_ranges, nk, a.scale, a.dk);
     sum(a.part_kv + nk, 2 * nk, a.dkv_ranges, nk, 1.f, a.dv);
@@ -879,6 +947,10 @@ static hipError_t launch_bwd(const BwdArgs& a, bool dense, hipStream_t stream) {
   const int64_t grid = stat_groups + (dense ? 0 : (int64_t)a.bh * a.n_words * chunks);
   if (grid > 0) attn_bwd_prepare_kernel<D><<<grid, 256, 0, stream>>>(a, stat_groups, chunks);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (a.list_min > 0) {
+    attn_bwd_pieces_kernel<<<((int64_t)a.bh * a.n_k + 31) / 32, 256, 0, stream>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   if (dense) return launch_passes<D, 4, true>(a, stream);
   return a.block == 64 ? launch_passes<D, 2, false>(a, stream) : launch_passes<D, 4, false>(a, stream);
 }

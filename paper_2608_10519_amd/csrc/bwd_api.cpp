@@ -20,6 +20,11 @@ extern "C" void sparstar_internal_bwd_plan(int B, int H, int64_t Lq, int64_t Lk,
   const BwdPlan p = attn_bwd_plan(int64_t(B) * H, Lq, Lk, D, block_size, dense != 0);
   out[0] = p.dq_ranges;
   out[1] = p.dkv_ranges;
+  if (p.slots > 0) {  // pieces of a key block that every query lists, if all lists are full
+    const int64_t nq = (Lq + block_size - 1) / block_size, nk = (Lk + block_size - 1) / block_size;
+    const int64_t most = attn_bwd_piece_max(int64_t(B) * H, nq, nk, block_size);
+    out[1] = (nq + most - 1) / most;
+  }
 }
 
 static int bwd_common(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o,
@@ -86,9 +91,19 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
   a.part_kv = reinterpret_cast<float*>(ws + plan.part_kv);
   a.dq_ranges = plan.dq_ranges;
   a.dkv_ranges = plan.dkv_ranges;
-  // (twice the lists' entries per key block, if every row fills its stride)
-  if (!dense && plan.rounds)
-    a.long_first = int(std::max<int64_t>(1, 2 * int64_t(a.n_q) * std::min(kv_stride, a.n_k) / a.n_k));
+  if (!dense && (plan.rounds || plan.slots > 0)) {
+    const int64_t entries = std::min(kv_stride, a.n_k);
+    a.piece_max = plan.slots > 0 ? attn_bwd_piece_max(bh, a.n_q, entries, block_size) : a.n_q;
+    // (in order of rounds: also those on twice as many lists as the average, if rows fill their stride)
+    if (plan.rounds) a.list_min = int(std::max<int64_t>(1, std::min<int64_t>(a.piece_max, 2 * a.n_q * entries / a.n_k)));
+    else if (a.piece_max < a.n_q) a.list_min = a.piece_max;
+    // blocks on more than twice the average are fewer than half, cut ones have 2 * extra pieces at most
+    a.most_pieces = (plan.rounds ? int(bh * a.n_k / 2) : 0) + (a.piece_max < a.n_q ? 2 * plan.extra : 0);
+    a.piece_count = reinterpret_cast<int32_t*>(ws + plan.count);
+    a.pieces = reinterpret_cast<int4*>(ws + plan.pieces);
+    a.listed = reinterpret_cast<uint8_t*>(ws + plan.listed);
+    a.part_piece = reinterpret_cast<float*>(ws + plan.part_piece);
+  }
   const hipError_t e = launch_attn_bwd(a, D, dense, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return report_error(SPARSTAR_ERR_HIP, hipGetErrorString(e));
   return clear_error();

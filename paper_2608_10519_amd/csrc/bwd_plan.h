@@ -13,8 +13,10 @@ namespace sparstar {
 
 struct BwdPlan {
   int dq_ranges, dkv_ranges;
+  int slots;    // partial results of pieces of key blocks (0: blocks are not cut)
+  int extra;    // pieces that there may be beyond one per block
   bool rounds;  // the dK/dV pass has more work-groups than the chip holds
-  size_t stats, bits, part, part_kv, total;  // byte offsets of the workspace's regions, and its size
+  size_t stats, bits, count, pieces, listed, part, part_kv, part_piece, total;  // byte offsets of the workspace's regions, and its size
 };
 
 constexpr int kBwdMaxRanges = 16;
@@ -42,6 +44,27 @@ inline int bwd_ranges(int64_t groups, int waves, int64_t tiles, double flops, do
   return best;
 }
 
+// The sparse dK/dV pass is not cut into ranges: some key blocks are on far more lists than
+// others (forced ones on all), and the pass would wait for those.  Instead a block is cut
+// that would take more than 1 / kPieceShare of what each of the work-groups that the chip
+// holds at a time has to do, into pieces of no more than that, and of kPieceRows query rows
+// or more: pieces cost partial results.  As entries / piece_max <= kPieceShare held, whatever
+// the lists, pieces take kPieceShare held work-groups beyond one per block at most, and cut
+// blocks have at most twice as many pieces.  5 heads of 70,409 x 2,634, D = 64, block 128,
+// budget 0.1: 231 us, whole blocks 683; 3 heads of 9,013 x 30,247, budget 0.05: 195 and 270;
+// 24 heads of 11,520 x 84,032, budget 0.25, where nothing is cut: 10.5 ms.
+constexpr int kPieceShare = 2;
+constexpr int kPieceRows = 1024;
+
+// Work-groups of the pass that the chip runs at full rate (four waves per CU).
+inline int bwd_held(int block) { return 1024 / (block / 32); }
+
+// The most lists per piece, for bh heads of n_q lists of `entries` at most.
+inline int attn_bwd_piece_max(int64_t bh, int64_t nq, int64_t entries, int block) {
+  const double share = double(bh) * double(nq) * double(entries) / (double(kPieceShare) * bwd_held(block));
+  return (int)std::min(std::max(ceil(share), double(kPieceRows / block)), 1e9);
+}
+
 inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, bool dense) {
   const int rows = dense ? 128 : block;
   const int64_t nq = (lq + block - 1) / block, nk = (lk + block - 1) / block;
@@ -51,19 +74,26 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   BwdPlan p{};
   p.dq_ranges = bwd_ranges(std::max<int64_t>(1, q_groups), rows / 32, (lk + 31) / 32, 3.0 * products,
                            4.0 * bh * lq * d);
-  p.dkv_ranges = bwd_ranges(k_groups, rows / 32, (lq + 31) / 32, 4.0 * products,
-                            8.0 * bh * lk * d);
-  // (the sparse walk is cut at whole words of 32 query blocks)
-  if (!dense) p.dkv_ranges = (int)std::min<int64_t>(p.dkv_ranges, std::max<int64_t>(1, (nq + 31) / 32));
-  p.rounds = k_groups * p.dkv_ranges > 256 * (d == 128 ? 4 : 8) / (rows / 32);
+  p.dkv_ranges = dense ? bwd_ranges(k_groups, rows / 32, (lq + 31) / 32, 4.0 * products, 8.0 * bh * lk * d) : 1;
+  p.rounds = lq > 0 && k_groups * (rows / 32) > (d == 128 ? 1024 : 2048);
+  if (!dense && lq >= 2 * kPieceRows) {
+    p.extra = kPieceShare * bwd_held(block);
+    const double most = double(bh * nk) * double((nq + kPieceRows / block - 1) / (kPieceRows / block));
+    p.slots = (int)std::min(2.0 * p.extra, most);
+  }
   auto align = [](size_t x) { return (x + 255) & ~size_t(255); };
   p.stats = 0;
   p.bits = align(size_t(bh * nq * block) * 2 * sizeof(float));
-  p.part = p.bits + (dense ? 0 : align(size_t(bh * nk * ((nq + 31) / 32)) * sizeof(uint32_t)));
+  p.count = p.bits + (dense ? 0 : align(size_t(bh * nk * ((nq + 31) / 32)) * sizeof(uint32_t)));
+  const bool list = !dense && (p.rounds || p.slots > 0);
+  p.pieces = p.count + (list ? 256 : 0);
+  p.listed = p.pieces + (list ? align(size_t(bh * nk + p.extra) * 16) : 0);
+  p.part = p.listed + (list ? align(size_t(bh * nk)) : 0);
   const size_t dq = p.dq_ranges > 1 ? size_t(bh * lq * d) * p.dq_ranges * sizeof(float) : 0;
   const size_t dkv = p.dkv_ranges > 1 ? 2 * size_t(bh * lk * d) * p.dkv_ranges * sizeof(float) : 0;
   p.part_kv = p.part + align(dq);
-  p.total = p.part_kv + dkv;
+  p.part_piece = p.part_kv + align(dkv);
+  p.total = p.part_piece + 2 * size_t(p.slots) * block * d * sizeof(float);
   return p;
 }
 

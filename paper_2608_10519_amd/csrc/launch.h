@@ -160,7 +160,14 @@ struct BwdArgs {
   int n_words;                   // ceil(n_q / 32)
   float *part, *part_kv;         // fp32 partial results of the ranges: dQ; dK and dV
   int dq_ranges, dkv_ranges;     // ranges of each list's keys, and of the queries; 1: results go out at once
-  int long_first;                // key blocks on more lists than this go first (sparse only; 0: in order)
+  // Key blocks on more than list_min lists come first, in pieces of piece_max lists at most
+  // (sparse only; list_min == 0: all blocks are taken in order and whole).
+  int list_min, piece_max;
+  int32_t* piece_count;          // entries of `pieces`, and of them such with a partial result
+  int4* pieces;                  // block's index in [BH, n_k], piece, pieces of the block, its first partial result
+  uint8_t* listed;               // [BH, n_k]: whether the block is among `pieces`
+  int most_pieces;               // no more entries than this, whatever the lists
+  float* part_piece;             // partial results: [.., 2, block, D]
 };
 
 // The 8-bit key/value cache (cache.hip): e4m3 codes [BH, cap, D] and scale bytes

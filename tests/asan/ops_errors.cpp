@@ -69,6 +69,23 @@ hipError_t launch_attn_bwd(const BwdArgs& a, int d, bool dense, hipStream_t) {
   if (!dense) CHECK(inside(a.bits, 4.0 * a.bh * a.n_k * a.n_words));
   if (!dense) CHECK((char*)a.stats + size_t(double(a.bh) * a.n_q * a.block * 8) <= (char*)a.bits);
   CHECK(a.dq_ranges >= 1 && a.dkv_ranges >= 1);
+  if (a.list_min > 0) {
+    // The lists hold `entries` at most.  A block with c > piece_max of them is cut into ceil(c / piece_max) < 2 c /
+    // piece_max pieces, at most c / piece_max beyond the first; one with c > list_min is taken whole.
+    const double entries = double(a.bh) * a.n_q * std::min(a.stride, a.n_k), blocks = double(a.bh) * a.n_k;
+    const bool cut = a.n_q > a.piece_max;
+    const double pieces =
+        cut ? std::min(2 * entries / a.piece_max, blocks * ((a.n_q + a.piece_max - 1) / a.piece_max)) : 0;
+    const double extra = cut ? std::min(entries / a.piece_max, pieces) : 0;
+    const double whole = a.list_min < a.piece_max ? floor(entries / (a.list_min + 1)) : 0;
+    CHECK(!dense && a.dkv_ranges == 1 && a.piece_max >= a.list_min && pieces + whole <= a.most_pieces);
+    CHECK((char*)a.bits + size_t(4.0 * a.bh * a.n_k * a.n_words) <= (char*)a.piece_count);
+    CHECK((char*)(a.piece_count + 2) <= (char*)a.pieces && reinterpret_cast<uintptr_t>(a.pieces) % 16 == 0);
+    CHECK((char*)a.pieces + size_t(16.0 * (blocks + extra)) <= (char*)a.listed);
+    CHECK((char*)a.listed + size_t(blocks) <= (char*)a.part);
+    CHECK((char*)a.part_kv <= (char*)a.part_piece);
+    CHECK(inside(a.part_piece, 8.0 * pieces * a.block * d));
+  }
   if (a.dq_ranges > 1) CHECK(inside(a.part, 4.0 * a.bh * lq * d * a.dq_ranges));
   if (a.dkv_ranges > 1) CHECK(inside(a.part_kv, 8.0 * a.bh * lk * d * a.dkv_ranges));
   // (the two may be in use at the same time)

@@ -42,6 +42,10 @@ GRADS = [
     (64, 64, 2, 12, 1000, 4001, 0.3, 1),
     (128, 64, 2, 8, 1500, 6001, None, 0),
     (64, 64, 2, 8, 1500, 6001, None, 0),
+    # (few key blocks, cut into many pieces; the last one of 60 keys)
+    (64, 128, 1, 2, 9001, 700, 0.2, 2),
+    (128, 64, 2, 1, 8200, 700, 0.2, 1),
+    (128, 128, 1, 3, 5000, 2000, 1.0, 0),
 ]
 
 
@@ -77,6 +81,48 @@ def test_gradients_of_many_work_groups(gpu_lib, case):
             want, tol = R.backward(*x, masks[b, h], scale, do[b, h].double(), dlse[b, h].double())
             for got, w, t, name in zip(grads, want, tol, ("dq", "dk", "dv")):
                 R.close(got[b, h], w.cpu(), t.cpu(), f"{name}[{b},{h}]")
+
+
+@pytest.mark.parametrize("D,block,H,Lq,Lk", [(64, 128, 2, 6000, 700), (128, 64, 6, 2500, 9001)])
+def test_cut_blocks_give_the_same_bits(gpu_lib, D, block, H, Lq, Lk):
+    """Call after call, in a workspace of garbage, and in a graph that is replayed with eager
+    work in between: the order in which blocks are listed changes nothing."""
+    assert bwd_plan(gpu_lib.load(), 1, H, Lq, Lk, D, block, False)[1] > 1
+    g = torch.Generator().manual_seed(Lq)
+    q, do = (torch.randn(1, H, Lq, D, generator=g).bfloat16().cuda() for _ in range(2))
+    k, v = (torch.randn(1, H, Lk, D, generator=g).bfloat16().cuda() for _ in range(2))
+    n_q, n_k = -(-Lq // block), -(-Lk // block)
+    num, idx = lists_to_device(lists_with_common_blocks(g, 1, H, n_q, n_k, 0.1, 2), n_q)
+    o, lse = gpu_lib.sparstar_sparse_attn_fwd(q, k, v, num, idx, block)
+    out = tuple(torch.empty_like(t) for t in (q, k, v))
+    need = gpu_lib.sparstar_attn_bwd_workspace_bytes(1, H, Lq, Lk, D, block)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def step():
+        gpu_lib.sparstar_sparse_attn_bwd(q, k, v, o, lse, do, num, idx, block, out=out, workspace=ws)
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in out]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        step()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+    torch.cuda.synchronize()
+    for rep in range(4):
+        for t in out:
+            t.fill_(math.nan)
+        ws.fill_(0x5a)
+        torch.cuda.synchronize()
+        graph.replay() if rep % 2 else step()
+        torch.cuda.synchronize()
+        _say(f"[bwd pieces] {Lq}x{Lk} {rep}")
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert math.isfinite(float(torch.randn(1 << 18, device="cuda").sum()))
 
 
 def test_common_blocks_are_begun_first(gpu_lib):
