@@ -14,6 +14,9 @@
  *      (Eq. 4-6);
  *   4. runs forward-only attention over the selected key blocks (Eq. 7,
  *      Section 5.3), writing O and the log-sum-exp.
+ * Beside it, over the same block lists: the gradients of that attention, for a
+ * generator that is trained under the mask, and the attention over keys and
+ * values held in 8 bits, for one whose cache outlives a scale.
  *
  * Conventions shared by every call
  *   - Tensors are dense, row-major, in device memory (HBM):
@@ -318,8 +321,8 @@ int sparstar_token_topk_mass(const void* q, const void* k, int B, int H, int64_t
 
 /*
  * Bytes of device scratch the gradient calls below need: two fp32 values per query
- * row, one bit per (key block, query block) pair, and, where a call of these sizes
- * is cut into ranges, their fp32 partial results.  0 for invalid sizes.
+ * row, one bit per (key block, query block) pair, a list of the key blocks, and, where
+ * a call of these sizes may be cut up, fp32 partial results.  0 for invalid sizes.
  */
 size_t sparstar_attn_bwd_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size);
 
@@ -331,7 +334,9 @@ size_t sparstar_attn_bwd_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, i
  *   dV_u = sum_t P_tu dO_t,   dK_u = s sum_t dS_tu q_t,   dQ_t = s sum_u dS_tu k_u.
  * Sums are held in fp32; P and dS are rounded to bf16 once, as operands of the
  * products, and the results to bf16 once.  The call is deterministic.
- *   q, k, v, B, H, Lq, Lk, D, block_size, softmax_scale   as for the forward
+ *   q, k, v, B, H, Lq, Lk, D, block_size   as for the forward
+ *   softmax_scale   as for the forward; between 0 and 1e-30 it is refused (lse / s
+ *                   has to stay finite)
  *   kv_num_blocks, kv_indices, kv_stride   the forward's lists.  (Malformed lists
  *                   give unspecified values but no out-of-range access; an entry
  *                   named twice in a row is one key block for dK and dV.)
@@ -403,7 +408,8 @@ int sparstar_cache_read(const void* k_cache, const void* v_cache, const uint8_t*
 
 /*
  * Bytes of device workspace that lets the calls below cut each list into ranges and
- * join their partial results; 0 where these sizes are never cut, or invalid.
+ * join their partial results, whatever the lists hold; 0 where these sizes are never
+ * cut, or invalid.
  */
 size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size);
 

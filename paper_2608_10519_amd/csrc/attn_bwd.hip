@@ -18,17 +18,24 @@
 //
 // The key groups find their query blocks in a bit matrix, one bit per (key block,
 // query block), that a small kernel builds from the lists.
+//
+// What bounds it: the matrix products, 14 D operations per pair of query and key where 10
+// would do in one pass, at the clock that the chip holds under them (1.55 GHz in the dense
+// dQ pass, its matrix cores busy 77% of the cycles; 1.81 GHz and 61% in dK/dV; a large
+// library product 1.85 and 70%).  24 dense heads of 2,880 x 75,392: 7.64 ms, 1.22 PFLOP/s
+// executed, of 1.29 that a large product reaches; 3 heads of 72,000 x 144,512 at 9.4%, block
+// 128: 4.8 ms, 1.14 PFLOP/s; at D = 64, where an element's softmax serves half the products,
+// 0.92 PFLOP/s (2 x 3 heads of 11,001 x 31,818, 1.01 ms).
 #include "attn_device.h"
 
 namespace sparstar {
 
-// Tiles of 32 or 64 rows.  Rows are stored unpadded in LDS and their 16-byte chunks XOR-permuted by swz(row), which leaves both reads of a
-// tile free of bank conflicts: 16 consecutive rows of one chunk (ds_read_b128), and
-// four consecutive rows of four chunks (the transpose read).
-template <int D, int ROWS = attn_tile_keys(D)>
+// Tiles of 32 rows.  Rows are stored unpadded in LDS and their 16-byte chunks XOR-permuted
+// by swz(row), which leaves both reads of a tile free of bank conflicts: 16 consecutive rows
+// of one chunk (ds_read_b128), and four consecutive rows of four chunks (the transpose read).
+template <int D>
 struct BwdCfg {
-  static constexpr int KB = ROWS;               // rows per tile
-  static constexpr int KT = KB / 32;            // 32-row sub-tiles
+  static constexpr int KB = 32;                 // rows per tile
   static constexpr int DS = D / 16;             // MFMA k-steps over D
   static constexpr int DT = D / 32;             // 32-row tiles of a D-row result
   static constexpr int RB = D * 2;              // bytes per row
@@ -256,8 +263,8 @@ __global__ __launch_bounds__(256) void attn_bwd_prepare_kernel(BwdArgs a, int64_
 // one query), then dQ^T += K^T dS^T with dS rounded to bf16 once.  The step is that of
 // the dK/dV pass below: S and dP of tile t + 1, then dQ of tile t, 24 MFMAs at D = 128.
 template <int D>
-struct DqCfg : BwdCfg<D, 32> {
-  using B = BwdCfg<D, 32>;
+struct DqCfg : BwdCfg<D> {
+  using B = BwdCfg<D>;
   static constexpr int NA = 2 * B::DS, NB = 2 * B::DT, NM = NA + NB;  // MFMAs of a step
   static constexpr int SPREAD = NA + B::DT - 1;    // MFMAs that the softmax is spread over
   static constexpr int P = 4;                      // MFMAs between an operand's read and its use
@@ -537,8 +544,8 @@ __device__ __forceinline__ void attn_bwd_dq(const BwdArgs& a, DqLds<D>& lds, uin
 // with 340 of them, kept the matrix cores busy 48% of the time, LDS at a quarter of its
 // rate).
 template <int D>
-struct DkvCfg : BwdCfg<D, 32> {
-  using B = BwdCfg<D, 32>;
+struct DkvCfg : BwdCfg<D> {
+  using B = BwdCfg<D>;
   static constexpr int NA = 2 * B::DS, NB = 4 * B::DT, NM = NA + NB;  // MFMAs of a step
   static constexpr int SPREAD = NM * 11 / 16;      // MFMAs that the softmax is spread over
   static constexpr int P = 6;                      // MFMAs between an operand's read and its use

@@ -8,8 +8,10 @@
 // top binade is used whole; a free fp32 scale would gain less than one binade at the
 // small end of a range of 17.
 //
-// Both kernels stream: the write reads 2 bytes and writes 1 per element, the read the
-// reverse.
+// Both kernels stream and are bound by memory: the write reads 2 bytes and writes 1 per
+// element, the read the reverse.  24 heads, D = 128, K and V: 11,520 tokens written in 37 us
+// (5.7 TB/s, some of it from the last-level cache), 84,032 read in 256 us (6.0 TB/s; a large
+// copy reaches 4.95); one token 7.6 us and 300 tokens read 10.7, which is the call itself.
 #include "device_common.h"
 
 namespace sparstar {
