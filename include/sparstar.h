@@ -389,6 +389,8 @@ int sparstar_dense_attn_bwd(const void* q, const void* k, const void* v, const v
  * where e = 120, the last value below bf16's end), NaN stays NaN.  Rows already in
  * a block that the call continues (block start <= row < first new row) keep their
  * values: e is at least theirs, and where it grows their codes are rounded to it.
+ * (The first call that touches a block starts at the block's first row, or finds a
+ * scale byte of 0, which holds no value up; codes need no initialisation.)
  * Rows behind the new ones count as empty: where a call ends inside a block, what
  * that block held from there on loses its meaning, and its bytes stay as they are.
  * No other block is touched.
@@ -418,7 +420,7 @@ size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk,
  * rows u < len_b of the blocks on its list, with the values that the codes stand for.
  * O and lse as there: bf16 queries, fp32 sums, P rounded to bf16 once.  Single tokens
  * (Lq of 1 to 32) take a path of their own that streams the cache.
- *   q, o            device bf16 [B,H,Lq,D];  lse device fp32 out [B,H,Lq], or NULL
+ *   q, o            device bf16 [B,H,Lq,D] (o may be q);  lse device fp32 out [B,H,Lq], or NULL
  *   k_cache .. v_scale, cap, block_size   the cache
  *   Lk              rows in use, 1 <= Lk <= cap (the bound of every len_b)
  *   lens            device int32 [B] or NULL: rows of each batch element, clamped to

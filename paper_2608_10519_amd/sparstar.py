@@ -370,6 +370,13 @@ def _launch(fn: str, device: torch.device, *args) -> None:
     _check(fn, rc)
 
 
+def _scratch(ws: torch.Tensor, device: torch.device) -> tuple[int, int]:
+    """(pointer, bytes) of a workspace."""
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _lists(num: torch.Tensor, idx: torch.Tensor, B: int, H: int, Lq: int, block_size: int,
            device: torch.device) -> tuple[int, int, int]:
     n_q = -(-Lq // block_size)
@@ -398,7 +405,7 @@ def _attn_bwd(fn, q, k, v, o, lse, d_o, lists, block_size, softmax_scale, dlse, 
         need = sparstar_attn_bwd_workspace_bytes(B, H, Lq, Lk, D, block_size)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
     _launch(fn, dev, q.data_ptr(), kp, vp, op, lp, dop, dlp, B, H, Lq, Lk, D, block_size, *listed,
-            float(softmax_scale), *grads, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+            float(softmax_scale), *grads, *_scratch(workspace, dev))
     return dq, dk, dv
 
 
@@ -432,9 +439,10 @@ class KvCache(NamedTuple):
 
     @classmethod
     def empty(cls, B: int, H: int, cap: int, D: int, block_size: int, device="cuda") -> "KvCache":
-        """An empty cache (its buffers need no initialisation)."""
+        """An empty cache.  Scale bytes of zero let a first write start inside a block; the
+        codes need no initialisation."""
         codes = [torch.empty((B, H, cap, D), dtype=torch.float8_e4m3fn, device=device) for _ in range(2)]
-        scales = [torch.empty((B, H, -(-cap // block_size)), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.zeros((B, H, -(-cap // block_size)), dtype=torch.uint8, device=device) for _ in range(2)]
         return cls(*codes, *scales, block_size)
 
 
@@ -507,7 +515,7 @@ def _cache_attn(fn, q, cache, lists, Lk, softmax_scale, lens, out, lse, return_l
             need = _cache_scratch(B, H, Lq, Lk, D, b, listed[2] if listed else 0)
             workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
         if workspace is not None:
-            wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+            wp, wn = _scratch(workspace, dev)
     _launch(fn, dev, q.data_ptr(), *ptrs, B, H, Lq, Lk, cap, D, b, lp, *listed, float(softmax_scale), op, lsep, wp, wn)
     return o, lse
 
