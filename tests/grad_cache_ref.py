@@ -54,7 +54,8 @@ def forward(q, k, v, mask, scale):
     """(o, lse, p) of one head in float64; a row without keys gets 0, -inf, 0."""
     s = (q @ k.t()) * scale
     s = s.masked_fill(~mask, -math.inf)
-    m = s.amax(dim=1, keepdim=True) if s.shape[1] else torch.full((s.shape[0], 1), -math.inf, dtype=s.dtype)
+    m = s.amax(dim=1, keepdim=True) if s.shape[1] else torch.full((s.shape[0], 1), -math.inf, dtype=s.dtype,
+                                                                       device=s.device)
     m = m.masked_fill(m == -math.inf, 0.0)
     e = (s - m).exp()
     l = e.sum(dim=1, keepdim=True)
@@ -88,7 +89,8 @@ def forward_tol(q, k, v, mask, scale):
     o, lse, p = forward(q, k, v, mask, scale)
     tol_o = (2 * U * (p @ v.abs()) + U * o.abs()) * SLACK + TINY
     D = q.shape[1]
-    mag = (q.abs() @ k.abs().t()).amax(dim=1) * scale if k.shape[0] else torch.zeros(q.shape[0], dtype=q.dtype)
+    mag = (q.abs() @ k.abs().t()).amax(dim=1) * scale if k.shape[0] else torch.zeros(q.shape[0], dtype=q.dtype,
+                                                                                          device=q.device)
     tol_lse = (D + 8) * 2.0 ** -24 * mag + 2.0 ** -20 * (1 + lse.abs().nan_to_num(posinf=0.0))
     return o, lse, tol_o, tol_lse
 

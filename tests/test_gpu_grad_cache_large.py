@@ -158,6 +158,11 @@ ATTEND = [
     (128, 64, 2, 12, 700, 7001, [7001, 33], 0.5, False),
     (64, 128, 1, 24, 2003, 4001, [4001], 1.0, False),
     (128, 64, 2, 6, 3003, 4001, [4001, 4000], None, False),
+    # (few rows: up to 64 ranges)
+    (128, 64, 1, 1, 64, 40_001, [40_001], None, False),
+    (64, 128, 2, 1, 100, 70_001, [70_001, 777], 0.5, False),
+    (128, 128, 1, 2, 190, 39_001, [0], None, False),
+    (64, 64, 1, 1, 33, 33_000, [32_999], 0.9, True),
 ]
 
 
