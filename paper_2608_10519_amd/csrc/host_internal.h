@@ -42,10 +42,16 @@ int check_attn_sizes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size
 extern "C" void sparstar_internal_attn_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                             int64_t kv_stride, int with_workspace, int64_t out[5]);
 
-// The cut of a gradient call (bwd_plan.h): key ranges of the dQ pass, query ranges of the
-// dK/dV pass; and of an attention call over the cache (cache_plan.h): waves per
-// work-group, ranges.  For tests.  kv_stride 0 is the dense call.
+// For tests: the cut of a gradient call (bwd_plan.h), key ranges of the dQ pass and query
+// ranges of the dK/dV pass (sparse: pieces of a key block that all of full lists name); and
+// of an attention call over the cache (cache_plan.h), waves of 32 query rows per work-group
+// and parts of a list that are joined.  kv_stride 0 is the dense call.
 extern "C" void sparstar_internal_bwd_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size, int dense,
                                            int64_t out[2]);
 extern "C" void sparstar_internal_cache_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                              int64_t kv_stride, int64_t out[2]);
+
+// Ranges of an attention call over the cache; with 1 it makes no use of a workspace, which
+// the Python binding then does not allocate.
+extern "C" int sparstar_internal_cache_ranges(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                              int64_t kv_stride);
