@@ -16,7 +16,8 @@ struct BwdPlan {
   int slots;    // partial results of pieces of key blocks (0: blocks are not cut)
   int extra;    // pieces that there may be beyond one per block
   bool rounds;  // the dK/dV pass has more work-groups than the chip holds
-  size_t stats, bits, count, pieces, listed, part, part_kv, part_piece, total;  // byte offsets of the workspace's regions, and its size
+  // byte offsets of the workspace's regions, and its size
+  size_t stats, bits, count, pieces, listed, part, part_kv, part_piece, total;
 };
 
 constexpr int kBwdMaxRanges = 16;
@@ -25,10 +26,9 @@ constexpr int kBwdMaxRanges = 16;
 // most.  A SIMD works off its waves at the rate of its matrix core whether it holds one or
 // two, so the pass takes as long as the SIMDs with the most of them: ceil(x) / x of the even
 // share, x waves per SIMD.  More ranges even that out (24 dense heads of 2,880 rows: 2.2
-// work-groups of 4 waves per CU; dQ takes 3.4 ms in 2 ranges and 3.0 in 4; one head of 72,000
-// rows, block 128: both gradients 2.37 ms in 1 and 1 ranges and 1.92 in 4 and 2) and cost
-// their partial results, `bytes` written and read again each, and a launch; both against a
-// time of the pass estimated from its operations.  A gain below 3 % is not worth the memory.
+// work-groups of 4 waves per CU; dQ takes 3.4 ms in 2 ranges and 3.0 in 4) and cost their
+// partial results, `bytes` written and read again each, and a launch; both against a time of
+// the pass estimated from its operations.  A gain below 3 % is not worth the memory.
 inline int bwd_ranges(int64_t groups, int waves, int64_t tiles, double flops, double bytes) {
   const double pass_us = flops / 1.1e9;
   int best = 1;
@@ -69,7 +69,7 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   const int rows = dense ? 128 : block;
   const int64_t nq = (lq + block - 1) / block, nk = (lk + block - 1) / block;
   const int64_t q_groups = bh * ((lq + rows - 1) / rows), k_groups = bh * ((lk + rows - 1) / rows);
-  // (the workspace does not depend on the lists: a quarter of the keys is taken for them)
+  // (the cut does not depend on the lists: a quarter of the keys is taken for them)
   const double products = 2.0 * d * double(bh) * double(lq) * double(lk) * (dense ? 1.0 : 0.25);
   BwdPlan p{};
   p.dq_ranges = bwd_ranges(std::max<int64_t>(1, q_groups), rows / 32, (lk + 31) / 32, 3.0 * products,
