@@ -222,22 +222,63 @@ __device__ __forceinline__ void list_bits(const BwdArgs& a, int64_t column, int 
   for (int j = threadIdx.x; j < hi - lo; j += 256) a.bits[(bh * a.n_k + lo + j) * a.n_words + word] = bits[j];
 }
 
-// ---- the key blocks that are taken first: 8 threads count a block's bits.  Where a block's
-// pieces stand in the list differs from call to call, what is computed for them does not.
+// ---- the key blocks that are taken first: 8 threads per block count its bits and cut it
+// where the rank of a bit, not its place, is a multiple of count / pieces: query blocks that
+// list a key block are often neighbours, and an even share of all query blocks would leave
+// one piece with most of the work.  Where a block's pieces stand in the list differs from
+// call to call, what is computed for them does not.
 __global__ __launch_bounds__(256) void attn_bwd_pieces_kernel(BwdArgs a) {
   const int64_t n = (int64_t)a.bh * a.n_k, i = (int64_t)blockIdx.x * 32 + threadIdx.x / 8;
+  const int t = threadIdx.x % 8;
+  const uint32_t* const words = a.bits + i * a.n_words;
   int count = 0;
   if (i < n)
-    for (int w = threadIdx.x % 8; w < a.n_words; w += 8) count += __builtin_popcount(a.bits[i * a.n_words + w]);
+    for (int w = t; w < a.n_words; w += 8) count += __builtin_popcount(words[w]);
 #pragma unroll
   for (int s = 4; s > 0; s /= 2) count += __shfl_xor(count, s, 8);
-  if (i >= n || threadIdx.x % 8 != 0) return;
-  a.listed[i] = count > a.list_min;
+  if (i >= n) return;
+  if (t == 0) a.listed[i] = count > a.list_min;
   if (count <= a.list_min) return;
   const int pieces = (count + a.piece_max - 1) / a.piece_max;
-  const int at = atomicAdd(a.piece_count, pieces);
-  const int slot = pieces > 1 ? atomicAdd(a.piece_count + 1, pieces) : 0;
-  for (int p = 0; p < pieces; ++p) a.pieces[at + p] = make_int4((int)i, p, pieces, slot);
+  int at = 0, slot = 0;
+  if (t == 0) {
+    at = atomicAdd(a.piece_count, pieces);
+    if (pieces > 1) slot = atomicAdd(a.piece_count + 1, pieces);
+  }
+  BwdPiece* const out = a.pieces + __shfl(at, 0, 8);
+  slot = __shfl(slot, 0, 8);
+  for (int p = t; p < pieces; p += 8) {
+    out[p].block = (int)i;
+    out[p].piece = p;
+    out[p].pieces = pieces;
+    out[p].slot = slot + p;
+  }
+  if (t == 0) {
+    out[0].begin = 0;
+    out[pieces - 1].end = a.n_q;
+  }
+  if (pieces == 1) return;
+  int before = 0;  // bits of the words before
+  for (int w0 = 0; w0 < a.n_words; w0 += 8) {
+    uint32_t left = w0 + t < a.n_words ? words[w0 + t] : 0u;
+    const int c = __builtin_popcount(left);
+    int upto = c;
+#pragma unroll
+    for (int s = 1; s < 8; s *= 2) {
+      const int x = __shfl_up(upto, s, 8);
+      if (t >= s) upto += x;
+    }
+    // pieces (but the first) that begin in this word, with the bit of rank count p / pieces
+    int rank = before + upto - c;
+    const int end = rank + c;
+    for (int64_t p = std::max<int64_t>(1, ((int64_t)rank * pieces + count - 1) / count); p < pieces; ++p) {
+      const int r = (int)((int64_t)count * p / pieces);
+      if (r >= end) break;
+      for (; rank < r; ++rank) left &= left - 1;
+      out[p].begin = out[p - 1].end = 32 * (w0 + t) + __builtin_ctz(left);
+    }
+    before += __shfl(upto, 7, 8);
+  }
 }
 
 // Statistics and bits in one launch: the first `stat_groups` work-groups take the rows.
@@ -574,16 +615,18 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
   // (The grid holds the pieces, as many as there can be, and every block; a block among the
   // pieces returns here, and so do work-groups past the end.)
   int slot = -1, range = 0, ranges = a.dkv_ranges, kg;
+  int b0 = 0, b1 = a.n_q;  // (sparse) the query blocks that the walk is about
   int64_t bh;
   if (!DENSE && a.list_min > 0) {
     const int first = __builtin_amdgcn_readfirstlane(*a.piece_count);
     int item = (int)index - first;
     if (item < 0) {
-      const int4 p = a.pieces[index];
-      item = __builtin_amdgcn_readfirstlane(p.x);
-      range = __builtin_amdgcn_readfirstlane(p.y);
-      ranges = __builtin_amdgcn_readfirstlane(p.z);
-      slot = __builtin_amdgcn_readfirstlane(p.w) + range;
+      const BwdPiece p = a.pieces[index];
+      item = __builtin_amdgcn_readfirstlane(p.block);
+      ranges = __builtin_amdgcn_readfirstlane(p.pieces);
+      slot = __builtin_amdgcn_readfirstlane(p.slot);
+      b0 = __builtin_amdgcn_readfirstlane(p.begin);
+      b1 = __builtin_amdgcn_readfirstlane(p.end);
     } else if (item >= a.bh * (int)n_g || __builtin_amdgcn_readfirstlane((int)a.listed[item]) != 0) {
       return;
     }
@@ -613,7 +656,6 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
   // block's words, 64 words at a time in a VGPR.
   const uint32_t* words = nullptr;
   int wpos, wend;            // words (dense: tiles) still to load, end of the range
-  int b0 = 0, b1 = 0;        // the range's query blocks
   uint32_t wreg = 0, cur = 0;
   uint64_t full = 0;         // words of the batch that have bits left
   int wbase = 0, qb32 = 0, sub = SUB, blk = 0;
@@ -623,8 +665,6 @@ __device__ __forceinline__ void attn_bwd_dkv(const BwdArgs& a, DkvLds<D>& lds, u
     wend = (int)(n * (range + 1) / ranges);
   } else {
     words = a.bits + (bh * a.n_k + kg) * a.n_words;
-    b0 = (int)((int64_t)a.n_q * range / ranges);
-    b1 = (int)((int64_t)a.n_q * (range + 1) / ranges);
     wpos = b0 / 32;
     wend = (b1 + 31) / 32;
   }
@@ -898,10 +938,10 @@ template <int D>
 __global__ __launch_bounds__(256) void attn_bwd_piece_sum_kernel(BwdArgs a) {
   const int n = *a.piece_count, all = a.block * D;
   for (int w = blockIdx.x; w < 8 * n; w += kPieceSumGroups) {
-    const int4 p = a.pieces[w / 8];
-    if (p.y != 0 || p.z <= 1) continue;  // (a block's first piece stands for it)
-    const int64_t bh = p.x / a.n_k, kg = p.x - bh * a.n_k, left = a.lk - kg * a.block;
-    const float* part = a.part_piece + (int64_t)p.w * 2 * all;
+    const BwdPiece p = a.pieces[w / 8];
+    if (p.piece != 0 || p.pieces <= 1) continue;  // (a block's first piece stands for it)
+    const int64_t bh = p.block / a.n_k, kg = p.block - bh * a.n_k, left = a.lk - kg * a.block;
+    const float* part = a.part_piece + (int64_t)p.slot * 2 * all;
     const int valid = (int)(left < a.block ? left : a.block) * D;
     for (int i = (w % 8 * 256 + threadIdx.x) * 4; i < 2 * all; i += 8 * 256 * 4) {
       const bool is_v = i >= all;
@@ -909,7 +949,7 @@ __global__ __launch_bounds__(256) void attn_bwd_piece_sum_kernel(BwdArgs a) {
       if (at >= valid) continue;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-      for (int r = 0; r < p.z; ++r) {
+      for (int r = 0; r < p.pieces; ++r) {
         const float4 u = *reinterpret_cast<const float4*>(part + (int64_t)r * 2 * all + i);
         x.x += u.x, x.y += u.y, x.z += u.z, x.w += u.w;
       }

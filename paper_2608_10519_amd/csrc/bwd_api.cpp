@@ -27,6 +27,17 @@ extern "C" void sparstar_internal_bwd_plan(int B, int H, int64_t Lq, int64_t Lk,
   }
 }
 
+extern "C" void sparstar_internal_bwd_pieces(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                             int64_t kv_stride, int64_t* out) {
+  const int64_t bh = int64_t(B) * H, nq = (Lq + block_size - 1) / block_size, nk = (Lk + block_size - 1) / block_size;
+  const BwdPlan p = attn_bwd_plan(bh, Lq, Lk, D, block_size, false);
+  const BwdPieces c = attn_bwd_pieces(p, bh, nq, nk, std::min(kv_stride, nk), block_size);
+  out[0] = c.list_min;
+  out[1] = c.piece_max;
+  out[2] = int64_t(p.count);
+  out[3] = int64_t(p.pieces);
+}
+
 static int bwd_common(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o,
                       const float* d_lse, int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                       const int32_t* kv_num_blocks, const int32_t* kv_indices, int kv_stride, float softmax_scale,
@@ -92,15 +103,12 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
   a.dq_ranges = plan.dq_ranges;
   a.dkv_ranges = plan.dkv_ranges;
   if (!dense && (plan.rounds || plan.slots > 0)) {
-    const int64_t entries = std::min(kv_stride, a.n_k);
-    a.piece_max = plan.slots > 0 ? attn_bwd_piece_max(bh, a.n_q, entries, block_size) : a.n_q;
-    // (in order of rounds: also those on twice as many lists as the average, if rows fill their stride)
-    if (plan.rounds) a.list_min = int(std::max<int64_t>(1, std::min<int64_t>(a.piece_max, 2 * a.n_q * entries / a.n_k)));
-    else if (a.piece_max < a.n_q) a.list_min = a.piece_max;
-    // blocks on more than twice the average are fewer than half, cut ones have 2 * extra pieces at most
-    a.most_pieces = (plan.rounds ? int(bh * a.n_k / 2) : 0) + (a.piece_max < a.n_q ? 2 * plan.extra : 0);
+    const BwdPieces c = attn_bwd_pieces(plan, bh, a.n_q, a.n_k, std::min(kv_stride, a.n_k), block_size);
+    a.list_min = c.list_min;
+    a.piece_max = c.piece_max;
+    a.most_pieces = c.most_pieces;
     a.piece_count = reinterpret_cast<int32_t*>(ws + plan.count);
-    a.pieces = reinterpret_cast<int4*>(ws + plan.pieces);
+    a.pieces = reinterpret_cast<BwdPiece*>(ws + plan.pieces);
     a.listed = reinterpret_cast<uint8_t*>(ws + plan.listed);
     a.part_piece = reinterpret_cast<float*>(ws + plan.part_piece);
   }

@@ -52,7 +52,10 @@ inline int bwd_ranges(int64_t groups, int waves, int64_t tiles, double flops, do
 // the lists, pieces take kPieceShare held work-groups beyond one per block at most, and cut
 // blocks have at most twice as many pieces.  5 heads of 70,409 x 2,634, D = 64, block 128,
 // budget 0.1: 231 us, whole blocks 683; 3 heads of 9,013 x 30,247, budget 0.05: 195 and 270;
-// 24 heads of 11,520 x 84,032, budget 0.25, where nothing is cut: 10.5 ms.
+// 24 heads of 11,520 x 84,032, budget 0.25, where nothing is cut: 10.5 ms.  Pieces hold even
+// shares of a block's lists: where neighbouring query blocks list the same keys, 5 heads of
+// 70,409 x 2,634 take 221 us (cut at even shares of all query blocks, 304), 3 heads of
+// 72,000 x 9,000 at D = 128 422 (495).
 constexpr int kPieceShare = 2;
 constexpr int kPieceRows = 1024;
 
@@ -63,6 +66,22 @@ inline int bwd_held(int block) { return 1024 / (block / 32); }
 inline int attn_bwd_piece_max(int64_t bh, int64_t nq, int64_t entries, int block) {
   const double share = double(bh) * double(nq) * double(entries) / (double(kPieceShare) * bwd_held(block));
   return (int)std::min(std::max(ceil(share), double(kPieceRows / block)), 1e9);
+}
+
+// What the sparse dK/dV pass does with its key blocks (see BwdArgs), for lists of `entries` at most.
+struct BwdPieces {
+  int list_min, piece_max, most_pieces;
+};
+
+inline BwdPieces attn_bwd_pieces(const BwdPlan& p, int64_t bh, int64_t nq, int64_t nk, int64_t entries, int block) {
+  BwdPieces c{};
+  c.piece_max = p.slots > 0 ? attn_bwd_piece_max(bh, nq, entries, block) : int(nq);
+  // (in order of rounds: also those on twice as many lists as the average, if rows fill their stride)
+  if (p.rounds) c.list_min = int(std::max<int64_t>(1, std::min<int64_t>(c.piece_max, 2 * nq * entries / nk)));
+  else if (c.piece_max < nq) c.list_min = c.piece_max;
+  // blocks on more than twice the average are fewer than half, cut ones have 2 * extra pieces at most
+  c.most_pieces = (p.rounds ? int(bh * nk / 2) : 0) + (c.piece_max < nq ? 2 * p.extra : 0);
+  return c;
 }
 
 inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, bool dense) {
@@ -87,7 +106,7 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   p.count = p.bits + (dense ? 0 : align(size_t(bh * nk * ((nq + 31) / 32)) * sizeof(uint32_t)));
   const bool list = !dense && (p.rounds || p.slots > 0);
   p.pieces = p.count + (list ? 256 : 0);
-  p.listed = p.pieces + (list ? align(size_t(bh * nk + p.extra) * 16) : 0);
+  p.listed = p.pieces + (list ? align(size_t(bh * nk + p.extra) * sizeof(BwdPiece)) : 0);
   p.part = p.listed + (list ? align(size_t(bh * nk)) : 0);
   const size_t dq = p.dq_ranges > 1 ? size_t(bh * lq * d) * p.dq_ranges * sizeof(float) : 0;
   const size_t dkv = p.dkv_ranges > 1 ? 2 * size_t(bh * lk * d) * p.dkv_ranges * sizeof(float) : 0;

@@ -48,6 +48,10 @@ extern "C" void sparstar_internal_attn_plan(int B, int H, int64_t Lq, int64_t Lk
 // and parts of a list that are joined.  kv_stride 0 is the dense call.
 extern "C" void sparstar_internal_bwd_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size, int dense,
                                            int64_t out[2]);
+// What the sparse dK/dV pass lists: the counts above which key blocks are taken first and cut
+// (list_min, piece_max of BwdArgs), and where the workspace has the list's length and entries.
+extern "C" void sparstar_internal_bwd_pieces(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                             int64_t kv_stride, int64_t out[4]);
 extern "C" void sparstar_internal_cache_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                              int64_t kv_stride, int64_t out[2]);
 

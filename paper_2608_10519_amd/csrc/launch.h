@@ -142,6 +142,15 @@ struct TopkArgs {
 };
 
 // The attention's gradients (attn_bwd.hip).
+
+// A share of one key block's dK and dV: the query blocks [begin, end) of those that list it.
+struct alignas(16) BwdPiece {
+  int block;       // index in [BH, n_k]
+  int piece, pieces;
+  int slot;        // its partial result (pieces > 1)
+  int begin, end;
+};
+
 struct BwdArgs {
   const uint16_t *q, *o, *d_o;   // [BH, Lq, D] bf16
   const uint16_t *k, *v;         // [BH, Lk, D] bf16
@@ -160,11 +169,11 @@ struct BwdArgs {
   int n_words;                   // ceil(n_q / 32)
   float *part, *part_kv;         // fp32 partial results of the ranges: dQ; dK and dV
   int dq_ranges, dkv_ranges;     // ranges of each list's keys, and of the queries; 1: results go out at once
-  // Key blocks on more than list_min lists come first, in pieces of piece_max lists at most
+  // Key blocks on more than list_min lists come first, in even pieces of piece_max lists at most
   // (sparse only; list_min == 0: all blocks are taken in order and whole).
   int list_min, piece_max;
   int32_t* piece_count;          // entries of `pieces`, and of them such with a partial result
-  int4* pieces;                  // block's index in [BH, n_k], piece, pieces of the block, its first partial result
+  BwdPiece* pieces;
   uint8_t* listed;               // [BH, n_k]: whether the block is among `pieces`
   int most_pieces;               // no more entries than this, whatever the lists
   float* part_piece;             // partial results: [.., 2, block, D]
