@@ -110,3 +110,44 @@ def test_neighbouring_lists_are_cut_evenly(gpu_lib, D, block, H, Lq, Lk, most):
     again = S.sparstar_sparse_attn_bwd(q, k, v, o, lse, do, num, idx, block, workspace=ws)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(grads, again))
+
+
+@pytest.mark.parametrize("D,block,H,Lq,Lk", [(128, 64, 8, 1000, 5000), (64, 128, 9, 1300, 9001)])
+def test_blocks_on_many_lists_are_begun_first(gpu_lib, D, block, H, Lq, Lk):
+    """Blocks on more than twice the average count of lists come first, or all in order where
+    the stride says that no count is far above it: the same bits, and float64's values."""
+    S = gpu_lib
+    n_q, n_k = -(-Lq // block), -(-Lk // block)
+    g = torch.Generator().manual_seed(Lk)
+    q, do = (torch.randn(1, H, Lq, D, generator=g).bfloat16().cuda() for _ in range(2))
+    k, v = (torch.randn(1, H, Lk, D, generator=g).bfloat16().cuda() for _ in range(2))
+    lists = R.random_lists(g, 1, H, n_q, n_k, 0.1)
+    for rows in lists[0]:
+        for i, row in enumerate(rows):
+            rows[i] = sorted(set(row[:9]) | {0, n_k // 2, n_k - 1})  # three blocks on every list
+    num, idx = lists_to_device(lists, n_q)
+    assert idx.shape[-1] <= 12
+    few = torch.full((1, H, n_q, 12), -1, dtype=torch.int32, device="cuda")
+    many = torch.full((1, H, n_q, n_k), -1, dtype=torch.int32, device="cuda")
+    few[..., :idx.shape[-1]] = many[..., :idx.shape[-1]] = idx
+    scale = 1 / math.sqrt(D)
+    o, lse = forward64(q, k, v, lists, block, scale)
+    need = S.sparstar_attn_bwd_workspace_bytes(1, H, Lq, Lk, D, block)
+    grads = []
+    for stride, listed in ((few, True), (many, False)):
+        plan = pieces_plan(S.load(), 1, H, Lq, Lk, D, block, stride.shape[-1])
+        # three blocks of each head have n_q lists, and no block has more
+        assert (0 < plan[0] < n_q) if listed else plan[0] >= n_q
+        assert plan[1] >= n_q  # nothing is cut
+        ws = torch.full((need,), 0x5a, dtype=torch.uint8, device="cuda")
+        grads.append(S.sparstar_sparse_attn_bwd(q, k, v, o, lse, do, num, stride, block, workspace=ws))
+        torch.cuda.synchronize()
+        found = listed_pieces(ws, plan)
+        print(f"[bwd order] {H} x {Lq}x{Lk}: plan {plan[:2]}, {len(found)} listed", flush=True)
+        if listed:
+            assert {f[0] for f in found} >= {h * n_k + j for h in range(H) for j in (0, n_k // 2, n_k - 1)}
+            assert len(found) < H * n_k // 2 and all(f[1:3] == [0, 1] for f in found)
+        else:
+            assert not found
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+    gradients_match(grads[0], q, k, v, do, lists, block, scale)
