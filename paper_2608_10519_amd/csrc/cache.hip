@@ -18,6 +18,16 @@ namespace sparstar {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+// Work-groups are launched in rows of at most this many: a launch may have fewer than 2^32
+// threads along each axis.  (A loop over the rest in each of 65,536 work-groups took 299 us for
+// the 84,032 tokens above, and 3% more for the 11,520.)
+constexpr int64_t kCacheGridRow = 1 << 20;
+static dim3 cache_grid(int64_t n) {
+  const int64_t rows = (n + kCacheGridRow - 1) / kCacheGridRow;
+  return dim3((uint32_t)((n + rows - 1) / rows), (uint32_t)rows);
+}
+__device__ __forceinline__ int64_t cache_group() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // 2^e of a scale byte: the byte is the exponent field of the float
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -38,7 +48,8 @@ template <int D, int BLK>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
   constexpr int CPR = D / 8, N = BLK * CPR / 256;  // 8-value chunks per row, per thread
   __shared__ float red[4];
-  int64_t w = blockIdx.x;
+  int64_t w = cache_group();
+  if (w >= 2 * (int64_t)a.bh * a.n_blocks) return;
   const int blk_i = (int)(w % a.n_blocks);
   w /= a.n_blocks;
   const int64_t bh = w % a.bh;
@@ -119,7 +130,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteArgs a) {
 // One thread per 16 codes.
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
   const int64_t cpr = a.d / 16, per_bh = a.l * cpr, n = (int64_t)a.bh * per_bh;
-  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t i = cache_group() * 256 + threadIdx.x;
   // the first n threads take K where it is wanted, the next n (or the first) V
   const bool is_v = a.k_out == nullptr || i >= n;
   if (a.k_out != nullptr && is_v) i -= n;
@@ -144,7 +155,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadArgs a) {
 }
 
 hipError_t launch_cache_write(const CacheWriteArgs& a, int d, int block, hipStream_t stream) {
-  const int64_t grid = 2 * (int64_t)a.bh * a.n_blocks;
+  const dim3 grid = cache_grid(2 * (int64_t)a.bh * a.n_blocks);
   if (d == 128 && block == 64) cache_write_kernel<128, 64><<<grid, 256, 0, stream>>>(a);
   else if (d == 128) cache_write_kernel<128, 128><<<grid, 256, 0, stream>>>(a);
   else if (block == 64) cache_write_kernel<64, 64><<<grid, 256, 0, stream>>>(a);
@@ -154,7 +165,7 @@ hipError_t launch_cache_write(const CacheWriteArgs& a, int d, int block, hipStre
 
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream) {
   const int64_t n = (int64_t)a.bh * a.l * (a.d / 16) * ((a.k_out != nullptr) + (a.v_out != nullptr));
-  cache_read_kernel<<<(n + 255) / 256, 256, 0, stream>>>(a);
+  cache_read_kernel<<<cache_grid((n + 255) / 256), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
