@@ -36,6 +36,11 @@
  *     kernel surface at the caller's next synchronisation, as for any HIP
  *     work.  sparstar_last_error() describes the last non-OK return on the
  *     calling thread.
+ *   - A launch has fewer than 2^32 threads.  The gradient calls (up to 2^28 rows of Q in all at
+ *     D = 128 and 2^29 at 64, each head's rows rounded up to blocks, and 2^31 of K, rounded up
+ *     to 128) and the attention over the cache (2^24 heads of up to 32 rows, or 2^28 rows)
+ *     return SPARSTAR_ERR_INVALID_ARG for sizes that need more; the cache's write and read take
+ *     any size.
  *   - The library holds no state besides that thread-local message and the
  *     per-GPU scratch array of sparstar_score_blocks_static; calls on
  *     different streams may run concurrently, except that calls of

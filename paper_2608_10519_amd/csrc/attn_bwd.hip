@@ -197,7 +197,6 @@ __device__ __forceinline__ void row_stats(const BwdArgs& a, int64_t group) {
 
 // ---- the bit matrix: word w of key block j holds, bit i, whether query block
 // 32 w + i lists j.  One work-group per word column and up to kBitsChunk key blocks.
-constexpr int kBitsChunk = 8192;
 __device__ __forceinline__ void list_bits(const BwdArgs& a, int64_t column, int chunk, uint32_t* bits) {
   const int64_t bh = column / a.n_words;
   const int word = (int)(column - bh * a.n_words);

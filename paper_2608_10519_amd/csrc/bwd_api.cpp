@@ -112,6 +112,8 @@ static int bwd_common(const void* q, const void* k, const void* v, const void* o
     a.listed = reinterpret_cast<uint8_t*>(ws + plan.listed);
     a.part_piece = reinterpret_cast<float*>(ws + plan.part_piece);
   }
+  if (attn_bwd_threads(plan, bh, Lq, Lk, D, block_size, dense, a.most_pieces) >= int64_t(1) << 32)
+    return report_error(SPARSTAR_ERR_INVALID_ARG, "too many rows and heads for one call");
   const hipError_t e = launch_attn_bwd(a, D, dense, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return report_error(SPARSTAR_ERR_HIP, hipGetErrorString(e));
   return clear_error();

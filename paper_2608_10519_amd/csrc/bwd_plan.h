@@ -116,4 +116,15 @@ inline BwdPlan attn_bwd_plan(int64_t bh, int64_t lq, int64_t lk, int d, int bloc
   return p;
 }
 
+// Threads of the largest launch of a call, of which there may be fewer than 2^32 (launch_bwd).
+inline int64_t attn_bwd_threads(const BwdPlan& p, int64_t bh, int64_t lq, int64_t lk, int d, int block, bool dense,
+                                int64_t most_pieces) {
+  const int64_t rows = dense ? 128 : block, nq = (lq + block - 1) / block, nk = (lk + block - 1) / block;
+  const int64_t prepare = bh * nq * block * (d / 8) + (dense ? 0 : 256 * bh * ((nq + 31) / 32) * (nk / kBitsChunk + 1)) + 256;
+  const int64_t dq = bh * p.dq_ranges * ((lq + rows - 1) / rows) * 2 * rows;
+  const int64_t dkv = (bh * p.dkv_ranges * ((lk + rows - 1) / rows) + most_pieces) * 2 * rows;
+  const int64_t sum = bh * std::max(p.dq_ranges > 1 ? lq : 0, p.dkv_ranges > 1 ? lk : 0) * (d / 8) + 256;
+  return std::max({prepare, dq, dkv, sum, 8 * bh * nk + 256});
+}
+
 }  // namespace sparstar

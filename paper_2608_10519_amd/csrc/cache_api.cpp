@@ -129,6 +129,8 @@ static int cache_attn_common(const void* q, const void* k_cache, const void* v_c
     return report_error(SPARSTAR_ERR_INVALID_ARG, "softmax_scale must be finite");
   const CachePlan plan =
       cache_attn_plan(bh, Lq, Lk, D, block_size, dense ? 0 : kv_stride, dense, workspace != nullptr);
+  if (cache_attn_threads(plan, bh * Lq, D) >= int64_t(1) << 32)
+    return report_error(SPARSTAR_ERR_INVALID_ARG, "too many query rows and heads for one call");
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
     return report_error(SPARSTAR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (workspace &&

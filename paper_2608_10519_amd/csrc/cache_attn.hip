@@ -8,6 +8,7 @@
 // VALU (cache_attn_kernel); up to 32 rows, single tokens above all, they stream the cache
 // (cache_token_kernel).
 #include "attn_device.h"
+#include "cache_plan.h"
 
 namespace sparstar {
 
@@ -876,9 +877,8 @@ static hipError_t launch_mode(const CacheAttnArgs& a, int waves, hipStream_t str
   if (waves == 2) cache_attn_kernel<D, 2, DENSE><<<a.grid, 128, 0, stream>>>(a);
   else cache_attn_kernel<D, 4, DENSE><<<a.grid, 256, 0, stream>>>(a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  // (a group per 16 threads reads a range at a time; few rows fill the chip with 16 of them)
-  return (int64_t)a.bh * a.lq <= 4096 || a.ranges > kSplits ? launch_merge<D, 16>(a, stream)
-                                                            : launch_merge<D, 1>(a, stream);
+  return cache_join_groups(waves, (int64_t)a.bh * a.lq, a.ranges) > 1 ? launch_merge<D, 16>(a, stream)
+                                                                      : launch_merge<D, 1>(a, stream);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int d, int waves, bool dense, hipStream_t stream) {

@@ -67,6 +67,18 @@ inline CachePlan cache_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int 
   return c;
 }
 
+// Groups of threads that share the join of a row's ranges (cache_merge_kernel): a group per D / 8
+// threads reads a range at a time, few rows fill the chip with 16 of them.
+inline int cache_join_groups(int waves, int64_t rows, int ranges) {
+  return waves == 1 || rows <= 4096 || ranges > kSplits ? 16 : 1;
+}
+
+// Threads of the largest launch of a call, of which there may be fewer than 2^32.
+inline int64_t cache_attn_threads(const CachePlan& p, int64_t rows, int d) {
+  const int64_t join = p.ranges > 1 ? rows * (d / 8) * cache_join_groups(p.waves, rows, p.ranges) + 256 : 0;
+  return std::max(p.grid * 64 * (p.waves == 1 ? kTokenWaves : p.waves), join);
+}
+
 inline size_t cache_part_o_bytes(int64_t rows, int d, int ranges) {
   return (size_t(rows * d) * ranges * 2 + 255) & ~size_t(255);
 }

@@ -151,6 +151,9 @@ struct alignas(16) BwdPiece {
   int begin, end;
 };
 
+// Key blocks per work-group of the bit matrix, each a word in LDS.
+constexpr int kBitsChunk = 8192;
+
 struct BwdArgs {
   const uint16_t *q, *o, *d_o;   // [BH, Lq, D] bf16
   const uint16_t *k, *v;         // [BH, Lk, D] bf16
