@@ -85,7 +85,7 @@ __device__ __forceinline__ void dma_tile(uint32_t m0, const uint32_t* voff, i32x
         "s_mov_b32 m0, %0\n\t"
         "s_nop 0\n\t"
         "buffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds"
+        "buffer_load_dwordx4 %2, %3, 0 offen offset:0x400 lds"
         :
         : "s"(m0), "v"(voff[0]), "v"(voff[1]), "s"(rsrc)
         : "memory", "m0");
@@ -94,8 +94,8 @@ __device__ __forceinline__ void dma_tile(uint32_t m0, const uint32_t* voff, i32x
         "s_mov_b32 m0, %0\n\t"
         "s_nop 0\n\t"
         "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
-        "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
+        "buffer_load_dwordx4 %2, %5, 0 offen offset:0x400 lds\n\t"
+        "buffer_load_dwordx4 %3, %5, 0 offen offset:0x800 lds\n\t"
         "buffer_load_dwordx4 %4, %5, 0 offen offset:0xc00 lds"
         :
         : "s"(m0), "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(rsrc)
