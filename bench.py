@@ -38,7 +38,7 @@ if ROOT not in sys.path:
 METRIC = "ms and effective TFLOP/s per sparse attention call at 72k-query 720p scale"
 PEAK_BF16_TFLOPS = 2500.0   # MI355X dense bf16 MFMA
 TRAFFIC_SUMMARY = os.path.join(ROOT, "profiles", "attn_fwd_sparse_720p_hbm.md")
-ATTN_SOURCE = os.path.join(ROOT, "paper_2608_10519_amd", "csrc", "attn_fwd.hip")
+CSRC = os.path.join(ROOT, "paper_2608_10519_amd", "csrc")
 
 
 def log(msg: str) -> None:
@@ -59,13 +59,35 @@ def executed_flops(num_blocks: np.ndarray, last_entries: np.ndarray, lq: int, lk
     return float((keys * rows).sum()) * 4.0 * d
 
 
+def attention_sources() -> list[str]:
+    """What decides the sparse attention kernel's traffic: its source, the plan that
+    cuts its calls, and every header of this library that they include."""
+    todo, found = ["attn_fwd.hip", "attn_plan.h"], []
+    while todo:
+        name = todo.pop(0)
+        if name in found:
+            continue
+        found.append(name)
+        with open(os.path.join(CSRC, name)) as f:
+            todo += re.findall(r'^#include "([^"]+)"', f.read(), re.M)
+    return found
+
+
+def attention_source_hash() -> str:
+    h = hashlib.sha256()
+    for name in attention_sources():
+        with open(os.path.join(CSRC, name), "rb") as f:
+            h.update(f.read())
+    return h.hexdigest()
+
+
 def traffic_from_profile() -> dict | None:
     """HBM bytes per launch of the sparse attention kernel from the committed
-    counter summary, if it was measured on the current kernel source."""
+    counter summary, if it was measured on the current sources."""
     if not os.path.exists(TRAFFIC_SUMMARY):
         return None
     text = open(TRAFFIC_SUMMARY).read()
-    src = hashlib.sha256(open(ATTN_SOURCE, "rb").read()).hexdigest()
+    src = attention_source_hash()
     m_sha = re.search(r"kernel_source_sha256:\s*([0-9a-f]{64})", text)
     m_f = re.search(r"fetch_bytes_per_launch:\s*([0-9.eE+]+)", text)
     m_w = re.search(r"write_bytes_per_launch:\s*([0-9.eE+]+)", text)
