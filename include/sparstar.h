@@ -423,8 +423,9 @@ size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk,
 /*
  * sparstar_sparse_attn_fwd over the cache: query token t of block i attends to the
  * rows u < len_b of the blocks on its list, with the values that the codes stand for.
- * O and lse as there: bf16 queries, fp32 sums, P rounded to bf16 once.  Single tokens
- * (Lq of 1 to 32) take a path of their own that streams the cache.
+ * O and lse as there: bf16 queries, fp32 sums, P rounded to bf16 once; where a workspace
+ * lets the call cut its lists, the ranges' sums are kept in fp16 in between (below).
+ * Single tokens (Lq of 1 to 32) take a path of their own that streams the cache.
  *   q, o            device bf16 [B,H,Lq,D] (o may be q);  lse device fp32 out [B,H,Lq], or NULL
  *   k_cache .. v_scale, cap, block_size   the cache
  *   Lk              rows in use, 1 <= Lk <= cap (the bound of every len_b)
@@ -433,10 +434,14 @@ size_t sparstar_cache_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk,
  *                   without rows gets O = 0 and lse = -inf.
  *   kv_num_blocks, kv_indices, kv_stride, softmax_scale   as for the bf16 forward;
  *                   a listed block past len_b adds nothing
- *   workspace       NULL for a single pass, or device scratch of at least
- *                   sparstar_cache_attn_workspace_bytes(...) bytes, 256-byte aligned,
- *                   no initialisation needed, garbage afterwards.  Calls that may
- *                   overlap in time need one each.
+ *   workspace       NULL for a single pass, whose sums stay in fp32 to the end, or device
+ *                   scratch of at least sparstar_cache_attn_workspace_bytes(...) bytes,
+ *                   256-byte aligned, no initialisation needed, garbage afterwards.
+ *                   Calls that may overlap in time need one each.  A range's
+ *                   unnormalised P V is kept there in fp16, times a power of two per row
+ *                   that brings its largest magnitude to [2^14, 2^15): off by at most
+ *                   2^-11 of the value once more, or 2^-39 of that magnitude where this
+ *                   is more.  Maxima, row sums and lse stay in fp32.
  * Heads that share keys and values: view Q of G such heads as [B, H / G, G Lq, D]
  * (with lists: where Lq is a whole number of blocks, or where G Lq rows share one).
  */

@@ -1,8 +1,9 @@
 // Attention over the 8-bit key/value cache (cache.hip), dense or over block lists.
 //
 // K and V stay 8-bit codes in memory, L2 and on the way into LDS: a tile moves half the
-// bytes of a bf16 one.  The only roundings are those of the bf16 forward: P to bf16 once,
-// O to bf16 once.
+// bytes of a bf16 one.  The roundings are those of the bf16 forward: P to bf16 once, O to
+// bf16 once, and in between, where a list is cut into ranges, each range's sums to fp16
+// (store_rows); all other sums are fp32.
 //
 // Two kernels.  Calls of more than 32 query rows are bound by the matrix cores and the
 // VALU (cache_attn_kernel); up to 32 rows, single tokens above all, they stream the cache

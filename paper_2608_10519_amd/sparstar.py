@@ -527,7 +527,7 @@ def sparstar_cache_sparse_attn_fwd(q, cache: KvCache, kv_num_blocks, kv_indices,
                                    workspace: torch.Tensor | None = None):
     """Block-sparse forward over the first Lk rows of the cache (all of it by default), or
     the first lens[b] of each batch element: returns (O, lse).  split=False runs a single
-    pass without a workspace."""
+    pass without a workspace, whose sums stay in fp32 (cut lists are joined from fp16 ones)."""
     return _cache_attn("sparstar_cache_sparse_attn_fwd", q, cache, (kv_num_blocks, kv_indices), Lk, softmax_scale,
                        lens, out, lse, return_lse, split, workspace)
 

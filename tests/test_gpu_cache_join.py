@@ -81,3 +81,36 @@ def test_every_part_is_joined(gpu_lib, case):
         want = seen(*x, lists[h], part_of[h], parts, block, 1 / math.sqrt(D))
         R.close(o[0, h], want[0], want[2], f"o[{h}]")
         R.close(lse[0, h], want[1], want[3], f"lse[{h}]")
+
+
+@pytest.mark.parametrize("split", [True, False])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"D{c[0]}b{c[1]}-{c[2]}-{c[3]}x{c[4]}-{c[5]}")
+def test_what_the_join_rounds(gpu_lib, case, split):
+    """All logits are zero, so that P is 1 and nothing is rounded but the ranges' sums A_r (to
+    fp16, by 2^-11, in a call that is cut) and O (to bf16, by 2^-8).  fp32 sums of up to 30,000
+    terms: 2^-24 of Sum |v| per addition, some 30 of them in a row per sub-tile and as many
+    levels above, far below 2^-16 of it.  Columns differ by up to 2^12 in size."""
+    S = gpu_lib
+    D, block, H, Lq, cap, stride = case
+    parts = cache_plan(S.load(), 1, H, Lq, cap, D, block, stride)[1]
+    _, k, v, lists, part_of = inputs(case, parts)
+    v = (v.float() * torch.exp2(-(torch.arange(D) % 13).float())).bfloat16()
+    c = S.KvCache.empty(1, H, cap, D, block)
+    S.sparstar_cache_write(k.cuda(), v.cuda(), c)
+    q = torch.zeros(1, H, Lq, D, dtype=torch.bfloat16)
+    if stride:
+        num, idx = lists_to_device([[[l] * -(-Lq // block) for l in lists]], -(-Lq // block))
+        o, lse = S.sparstar_cache_sparse_attn_fwd(q.cuda(), c, num, idx, split=split)
+    else:
+        o, lse = S.sparstar_cache_dense_attn_fwd(q.cuda(), c, split=split)
+    for h in range(H):
+        vd = values_of(c)[1][0, h]
+        n = int((part_of[h] >= 0).sum())
+        sums = torch.stack([vd[part_of[h] == p].sum(dim=0) for p in range(parts)])
+        want, size = sums.sum(dim=0) / n, vd[part_of[h] >= 0].abs().sum(dim=0) / n
+        kept = sums.abs().sum(dim=0) / n * 2.0 ** -11 + parts * float(sums.abs().max()) / n * 2.0 ** -39 if split else 0
+        inner = kept + 2.0 ** -16 * size
+        tol = (R.U * (want.abs() + inner) + inner).expand(Lq, D)
+        R.close(o[0, h], want.expand(Lq, D), tol, f"o[{h}]")
+        R.close(lse[0, h], torch.full((Lq,), math.log(n), dtype=torch.float64),
+                torch.full((Lq,), 2.0 ** -20 * (1 + math.log(n)), dtype=torch.float64), f"lse[{h}]")
