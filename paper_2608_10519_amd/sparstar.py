@@ -4,6 +4,10 @@ Each function mirrors the C entry point of the same name in include/sparstar.h.
 torch supplies device memory and the current HIP stream; every step of the
 computation runs in the library's HIP kernels.  There is no fallback: if the
 library cannot be loaded, every call raises.
+
+The calls stand outside torch's graph: their results have no history, also where
+inputs require gradients.  A torch.autograd.Function around a forward and the
+gradient call of the same name joins them (README.md has one).
 """
 from __future__ import annotations
 
