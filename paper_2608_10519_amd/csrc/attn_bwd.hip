@@ -25,7 +25,8 @@
 // library product 1.85 and 70%).  24 dense heads of 2,880 x 75,392: 7.64 ms, 1.22 PFLOP/s
 // executed, of 1.29 that a large product reaches; 3 heads of 72,000 x 144,512 at 9.4%, block
 // 128: 4.8 ms, 1.14 PFLOP/s; at D = 64, where an element's softmax serves half the products,
-// 0.92 PFLOP/s (2 x 3 heads of 11,001 x 31,818, 1.01 ms).
+// 1.08 (24 dense heads of 2,880 x 75,392, 4.32 ms, matrix cores 57% and 62% busy) and 0.92 (2 x
+// 3 heads of 11,001 x 31,818, 1.01 ms: lists of different lengths leave CUs idle 14% and 24%).
 #include "attn_device.h"
 
 namespace sparstar {
