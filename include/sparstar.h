@@ -16,7 +16,9 @@
  *      Section 5.3), writing O and the log-sum-exp.
  * Beside it, over the same block lists: the gradients of that attention, for a
  * generator that is trained under the mask, and the attention over keys and
- * values held in 8 bits, for one whose cache outlives a scale.
+ * values held in 8 bits, or in pages of 4-bit values, for one whose cache outlives
+ * a scale.  The rotation of queries and keys by their positions, and its gradient,
+ * stand before all of them.
  *
  * Conventions shared by every call
  *   - Tensors are dense, row-major, in device memory (HBM):
@@ -39,8 +41,8 @@
  *   - A launch has fewer than 2^32 threads.  The gradient calls (up to 2^28 rows of Q in all at
  *     D = 128 and 2^29 at 64, each head's rows rounded up to blocks, and 2^31 of K, rounded up
  *     to 128) and the attention over the cache (2^24 heads of up to 32 rows, or 2^28 rows)
- *     return SPARSTAR_ERR_INVALID_ARG for sizes that need more; the cache's write and read take
- *     any size.
+ *     return SPARSTAR_ERR_INVALID_ARG for sizes that need more; the caches' writes and reads and
+ *     the rotations take any size.
  *   - The library holds no state besides that thread-local message and the
  *     per-GPU scratch array of sparstar_score_blocks_static; calls on
  *     different streams may run concurrently, except that calls of
@@ -456,6 +458,165 @@ int sparstar_cache_dense_attn_fwd(const void* q, const void* k_cache, const void
                                   const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int64_t cap, int D,
                                   int block_size, const int32_t* lens, float softmax_scale, void* o, float* lse,
                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions.  A token at position t has each of its first 2 P channels turned with
+ * its partner by an angle of the token's own:
+ *   (a, b) -> (c a - s b, c b + s a),   (c, s) = table[t, p] = m (cos x_t,p, sin x_t,p),
+ * pair p being the channels (p, p + P) or, interleaved, (2 p, 2 p + 1).  Channels from 2 P
+ * on pass unchanged.  The table holds fp32; a turn is evaluated in fp64, where its products
+ * are exact, and rounded once to fp32 and bf16.
+ */
+
+/* Most pairs and axes of a table. */
+#define SPARSTAR_ROPE_MAX_PAIRS 64
+#define SPARSTAR_ROPE_MAX_AXES 4
+
+/*
+ * Angles per step of `pairs` pairs: f_p = base^(-p / pairs), p = 0 .. pairs - 1.  For
+ * sequences `factor` times as long as the `length` tokens that the frequencies were made
+ * for, a pair that turns r = length f_p / (2 pi) times over these keeps the share
+ * g = min(1, max(0, (r - slow) / (fast - slow))) of its frequency and gives up the rest:
+ * f_p (g + (1 - g) / factor).  Fast pairs tell near tokens apart and stay, slow ones are
+ * stretched.  Host only.
+ *   base            > 1, finite;  factor >= 1 (1: nothing is stretched, and length, slow
+ *                   and fast are ignored);  length > 0, 0 <= slow < fast
+ *   out             host [pairs] receives the frequencies, radians per step
+ * Returns SPARSTAR_OK or SPARSTAR_ERR_INVALID_ARG.
+ */
+int sparstar_rope_frequencies(int pairs, double base, double factor, double length, double slow, double fast,
+                              double* out);
+
+/*
+ * The table of a set of rows: table[t, p] = amplitude (cos x, sin x) with
+ * x = freq[p] coords[t, axis[p]], evaluated in fp64 (the angle off by at most 2^-51 |x|) and
+ * rounded to fp32.
+ *   coords          device int32 [rows, axes]: a token's place in time, height, width, ...
+ *   rows, axes      rows >= 0, 1 <= axes <= SPARSTAR_ROPE_MAX_AXES
+ *   pairs           1 .. SPARSTAR_ROPE_MAX_PAIRS
+ *   freq            HOST double [pairs], finite, |freq| <= 2^20
+ *   axis            HOST int32 [pairs], each in [0, axes); NULL: axis 0 for all
+ *   amplitude       finite
+ *   table           device fp32 out [rows, pairs, 2], 8-byte aligned
+ */
+int sparstar_rope_table(const int32_t* coords, int64_t rows, int axes, int pairs, const double* freq,
+                        const int32_t* axis, double amplitude, float* table, void* stream);
+
+/* Distances, in elements, between batch elements, heads and tokens of a [B, H, L, D] tensor
+ * whose rows of D channels are contiguous.  Those of a size of 1 are ignored. */
+typedef struct {
+  int64_t batch;
+  int64_t head;
+  int64_t token;
+} sparstar_strides;
+
+/*
+ * x [B, H, L, D] turned by its tokens' positions into y.  With strides, a slice of a fused
+ * projection [B, L, 3, H, D] goes straight into the [B, H, L, D] of the attention calls.
+ *   x, xs           device bf16 and its strides: multiples of 8, not negative (0: a
+ *                   broadcast input); 16-byte aligned
+ *   B, H, L, D      B, H >= 1, L >= 0, D 64 or 128
+ *   table, table_rows, pairs   device fp32 [table_rows, pairs, 2], 16-byte aligned; pairs a
+ *                   multiple of 8, 8 <= pairs <= D / 2; table_rows >= 1 (where L > 0)
+ *   interleaved     which channels make a pair (above)
+ *   positions       device int32 [B, L]: the table row of every token, or NULL: token i of
+ *                   every batch element is at start + i (0 <= start, start + L <=
+ *                   table_rows).  A position outside the table is moved to its end: values
+ *                   are unspecified, no access is out of range.
+ *   y, ys           device bf16 out, strides as for x but of rows that do not overlap.  y may
+ *                   be x, with the same strides; otherwise the two may not overlap.
+ */
+int sparstar_rope_fwd(const void* x, sparstar_strides xs, int B, int H, int64_t L, int D, const float* table,
+                      int64_t table_rows, int pairs, int interleaved, const int32_t* positions, int64_t start, void* y,
+                      sparstar_strides ys, void* stream);
+
+/* The gradient of x from the one of y: (a, b) -> (c a + s b, c b - s a).  x and y are exchanged:
+ * `dy` is the input, `dx` the output; arguments as above. */
+int sparstar_rope_bwd(const void* dy, sparstar_strides dys, int B, int H, int64_t L, int D, const float* table,
+                      int64_t table_rows, int pairs, int interleaved, const int32_t* positions, int64_t start,
+                      void* dx, sparstar_strides dxs, void* stream);
+
+/*
+ * The paged 4-bit key/value cache.  It holds, in the caller's buffers, n_pages pages of
+ * block_size tokens of all heads,
+ *   k_pages, v_pages   [n_pages, H, block_size, D / 2] bytes of two e2m1 codes, the even
+ *                      channel in the low half
+ *   k_scale, v_scale   [n_pages, H, block_size, D / 32] bytes e + 127, one for 32 channels of
+ *                      a token
+ * (all 16-byte aligned), and a value is code * 2^e with e in [-125, 125]: exact in bf16.  A code
+ * stands for 0, 1/2, 1, 3/2, 2, 3, 4 or 6 (0..7), negated in 8..15.  Scale byte 255 makes its
+ * 32 values NaN.  Row r of sequence b is row r % block_size of page
+ *   pages[b, r / block_size]     device int32 [B, n_table]
+ * A page may stand in the tables of several sequences, which then share its rows.  One
+ * outside [0, n_pages) does not exist: what would be written there is dropped, it reads as
+ * zeros, and attention leaves it out.
+ *
+ * sparstar_paged_write appends L tokens: token i of sequence b becomes row start + i, or
+ * starts[b] + i.
+ *   k, v            device bf16 [B, H, L, D] with strides as for sparstar_rope_fwd
+ *   start           first row for every sequence (0 <= start, start + L <= n_table *
+ *                   block_size)
+ *   starts          device int32 [B] or NULL: first row of each sequence instead of `start`.
+ *                   Tokens that would land outside its table's rows are dropped.
+ *   counts          device int32 [B] or NULL: only the sequence's first counts[b] tokens are
+ *                   written (clamped to [0, L]); a padded batch
+ *   table           NULL, or k is turned on the way as by sparstar_rope_fwd (the same bits as
+ *                   k rotated first), with table_rows, pairs, interleaved as there
+ *   positions       device int32 [B, L]: the table row of every token, or NULL: the row at
+ *                   which it lands (start + L <= table_rows).  Outside the table: as there.
+ * Per token, head and 32 channels, e is the least integer with amax 2^-e <= 6 over the finite
+ * values (e = -125 if they are all zero), and a code is the nearest value, ties to the even
+ * code: off by at most a quarter of the value, or 2^(e-2) where the value is below 2^e.
+ * What would exceed 6 * 2^125 saturates there, infinities at 6 * 2^e; a NaN makes its 32
+ * values NaN.  Only the rows of the tokens written change.  Two tokens of one call may not
+ * land in the same row of a page.
+ */
+int sparstar_paged_write(const void* k, sparstar_strides ks, const void* v, sparstar_strides vs, int B, int H,
+                         int64_t L, int D, int block_size, int64_t start, const int32_t* starts,
+                         const int32_t* counts, const float* table, int64_t table_rows, int pairs, int interleaved,
+                         const int32_t* positions, const int32_t* pages, int64_t n_table, int64_t n_pages,
+                         void* k_pages, void* v_pages, uint8_t* k_scale, uint8_t* v_scale, void* stream);
+
+/*
+ * Rows [start, start + L) of every sequence as bf16 again, exactly: k and v [B, H, L, D],
+ * device bf16 out, dense, 16-byte aligned, either of them NULL to leave it out.  For calls
+ * that take bf16 keys, such as sparstar_score_blocks.  0 <= start, start + L <= n_table *
+ * block_size.
+ */
+int sparstar_paged_read(const void* k_pages, const void* v_pages, const uint8_t* k_scale, const uint8_t* v_scale,
+                        int B, int H, int64_t start, int64_t L, int D, int block_size, const int32_t* pages,
+                        int64_t n_table, int64_t n_pages, void* k, void* v, void* stream);
+
+/*
+ * Bytes of device workspace that lets the calls below cut each list into ranges and join
+ * their partial results, whatever the lists hold; 0 where these sizes are never cut, or
+ * invalid.
+ */
+size_t sparstar_paged_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size);
+
+/*
+ * sparstar_cache_sparse_attn_fwd over the paged cache: query token t of block i attends to the
+ * rows u < len_b of the blocks on its list, with the values that the codes stand for.  Block
+ * j of sequence b is the page pages[b, j].  Arguments, roundings and results are those of the
+ * 8-bit cache's calls, but for
+ *   pages, n_table  device int32 [B, n_table], Lk <= n_table * block_size
+ *   workspace       of sparstar_paged_attn_workspace_bytes(...); up to 32 query rows the
+ *                   ranges' sums are kept in fp32 there, for more in fp16 as there
+ * and P, which is not rounded where a single row attends (Lq = 1).
+ */
+int sparstar_paged_sparse_attn_fwd(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
+                                   const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int D,
+                                   int block_size, const int32_t* pages, int64_t n_table, int64_t n_pages,
+                                   const int32_t* lens, const int32_t* kv_num_blocks, const int32_t* kv_indices,
+                                   int kv_stride, float softmax_scale, void* o, float* lse, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* The same over all rows of the cache; arguments as there. */
+int sparstar_paged_dense_attn_fwd(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
+                                  const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                  const int32_t* pages, int64_t n_table, int64_t n_pages, const int32_t* lens,
+                                  float softmax_scale, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                  void* stream);
 
 /* Message for the last non-OK return on this thread ("" if none). */
 const char* sparstar_last_error(void);

@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "libsparstar.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["host_api.cpp", "pool_score.hip", "select.hip", "attn_fwd.hip", "mass.hip", "static_scratch.hip",
-           "bwd_api.cpp", "attn_bwd.hip", "cache_api.cpp", "cache.hip", "cache_attn.hip"]
+           "bwd_api.cpp", "attn_bwd.hip", "cache_api.cpp", "cache.hip", "cache_attn.hip",
+           "rope_api.cpp", "rope.hip", "paged_api.cpp", "paged.hip", "paged_attn.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

@@ -40,6 +40,10 @@ class Range(ctypes.Structure):
     _fields_ = [("begin", ctypes.c_int64), ("end", ctypes.c_int64)]
 
 
+class Strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
 def load(path: str | None = None) -> ctypes.CDLL:
     """Load the HIP library (once).  Raises if it is not built."""
     global _lib
@@ -103,6 +107,28 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.sparstar_cache_dense_attn_fwd.argtypes = [c_p] * 5 + [c_i, c_i, c_i64, c_i64, c_i64, c_i, c_i, c_p, c_f, c_p,
                                                               c_p, c_p, c_sz, c_p]
     lib.sparstar_cache_dense_attn_fwd.restype = c_i
+    lib.sparstar_rope_frequencies.argtypes = [c_i] + [ctypes.c_double] * 5 + [c_dp]
+    lib.sparstar_rope_frequencies.restype = c_i
+    lib.sparstar_rope_table.argtypes = [c_p, c_i64, c_i, c_i, c_dp, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, c_p, c_p]
+    lib.sparstar_rope_table.restype = c_i
+    for fn in (lib.sparstar_rope_fwd, lib.sparstar_rope_bwd):
+        fn.argtypes = [c_p, Strides, c_i, c_i, c_i64, c_i, c_p, c_i64, c_i, c_i, c_p, c_i64, c_p, Strides, c_p]
+        fn.restype = c_i
+    lib.sparstar_paged_write.argtypes = [c_p, Strides, c_p, Strides, c_i, c_i, c_i64, c_i, c_i, c_i64, c_p, c_p, c_p,
+                                         c_i64, c_i, c_i, c_p, c_p, c_i64, c_i64, c_p, c_p, c_p, c_p, c_p]
+    lib.sparstar_paged_write.restype = c_i
+    lib.sparstar_paged_read.argtypes = [c_p] * 4 + [c_i, c_i, c_i64, c_i64, c_i, c_i, c_p, c_i64, c_i64, c_p, c_p, c_p]
+    lib.sparstar_paged_read.restype = c_i
+    lib.sparstar_paged_attn_workspace_bytes.argtypes = [c_i, c_i, c_i64, c_i64, c_i, c_i]
+    lib.sparstar_paged_attn_workspace_bytes.restype = c_sz
+    lib.sparstar_internal_paged_ranges.argtypes = [c_i, c_i, c_i64, c_i64, c_i, c_i, c_i64]
+    lib.sparstar_internal_paged_ranges.restype = c_i
+    lib.sparstar_paged_sparse_attn_fwd.argtypes = [c_p] * 5 + [c_i, c_i, c_i64, c_i64, c_i, c_i, c_p, c_i64, c_i64, c_p,
+                                                               c_p, c_p, c_i, c_f, c_p, c_p, c_p, c_sz, c_p]
+    lib.sparstar_paged_sparse_attn_fwd.restype = c_i
+    lib.sparstar_paged_dense_attn_fwd.argtypes = [c_p] * 5 + [c_i, c_i, c_i64, c_i64, c_i, c_i, c_p, c_i64, c_i64, c_p,
+                                                              c_f, c_p, c_p, c_p, c_sz, c_p]
+    lib.sparstar_paged_dense_attn_fwd.restype = c_i
     lib.sparstar_last_error.argtypes = []
     lib.sparstar_last_error.restype = ctypes.c_char_p
     lib.sparstar_clip_keep_ranges.argtypes = [c_i, Range, Range, c_rp, c_i]
@@ -543,3 +569,203 @@ def sparstar_cache_dense_attn_fwd(q, cache: KvCache, Lk: int | None = None, soft
     """Dense forward over the cache: returns (O, lse)."""
     return _cache_attn("sparstar_cache_dense_attn_fwd", q, cache, None, Lk, softmax_scale, lens, out, lse, return_lse,
                        split, workspace)
+
+
+# --------------------------------------------------------------------------
+# rotary positions
+# --------------------------------------------------------------------------
+def sparstar_rope_frequencies(pairs: int, base: float = 10_000.0, *, factor: float = 1.0, length: float = 0.0,
+                              slow: float = 1.0, fast: float = 32.0) -> list[float]:
+    """Radians per step of each pair; with factor > 1 those of pairs that turn slowly over
+    `length` tokens are stretched."""
+    out = (ctypes.c_double * max(pairs, 1))()
+    _check("sparstar_rope_frequencies", load().sparstar_rope_frequencies(pairs, base, factor, length, slow, fast, out))
+    return list(out)
+
+
+def sparstar_rope_table(coords: torch.Tensor, freq: Sequence[float], axis: Sequence[int] | None = None,
+                        amplitude: float = 1.0, *, out: torch.Tensor | None = None) -> torch.Tensor:
+    """amplitude (cos, sin) of freq[p] coords[t, axis[p]]: fp32 [rows, len(freq), 2] of int32
+    coordinates [rows, axes] on the GPU."""
+    if coords.dtype != torch.int32 or not coords.is_cuda or not coords.is_contiguous() or coords.dim() != 2:
+        raise ValueError("coords must be a contiguous 2-D int32 tensor on the GPU [rows, axes]")
+    if axis is not None and len(axis) != len(freq):
+        raise ValueError("freq and axis differ in length")
+    (rows, axes), pairs, dev = coords.shape, len(freq), coords.device
+    table = torch.empty((rows, pairs, 2), dtype=torch.float32, device=dev) if out is None else out
+    tp = _like(table, (rows, pairs, 2), torch.float32, "out", dev)
+    f = (ctypes.c_double * max(pairs, 1))(*freq)
+    ax = (ctypes.c_int32 * max(pairs, 1))(*axis) if axis is not None else None
+    _launch("sparstar_rope_table", dev, coords.data_ptr(), rows, axes, pairs, f, ax, float(amplitude), tp)
+    return table
+
+
+def _strided(t: torch.Tensor, name: str, device: torch.device | None = None, shape=None) -> Strides:
+    """Strides of a bf16 tensor [B, H, L, D] on the GPU whose rows are contiguous."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+        raise ValueError(f"{name} must be a 4-D bf16 tensor on the GPU [B, H, L, D] with contiguous rows")
+    if device is not None and (t.device != device or t.shape != shape):
+        raise ValueError(f"{name} must be a tensor on {device} of shape {tuple(shape)}")
+    return Strides(*t.stride()[:3])
+
+
+def _table(table: torch.Tensor, device: torch.device) -> tuple[int, int, int]:
+    """(pointer, rows, pairs) of a table."""
+    if table.dim() != 3:
+        raise ValueError("the table must be [rows, pairs, 2]")
+    return _like(table, (*table.shape[:2], 2), torch.float32, "table", device), table.shape[0], table.shape[1]
+
+
+def _rope(fn, x, table, start, positions, interleaved, out):
+    xs, dev = _strided(x, "x"), x.device
+    B, H, L, D = x.shape
+    tp, rows, pairs = _table(table, dev)
+    pp = _like(positions, (B, L), torch.int32, "positions", dev)
+    y = torch.empty((B, H, L, D), dtype=torch.bfloat16, device=dev) if out is None else out
+    ys = _strided(y, "out", dev, x.shape)
+    _launch(fn, dev, x.data_ptr(), xs, B, H, L, D, tp, rows, pairs, int(interleaved), pp, start, y.data_ptr(), ys)
+    return y
+
+
+def sparstar_rope_fwd(x: torch.Tensor, table: torch.Tensor, start: int = 0, *, positions: torch.Tensor | None = None,
+                      interleaved: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """x [B, H, L, D] turned by its tokens' positions: start + i, or positions[b, i] (int32),
+    rows of the table.  Pairs are channels p and p + P, or, interleaved, 2 p and 2 p + 1; those
+    past 2 P pass.  x may be a slice of a fused projection; the result is dense, or `out`,
+    which may be x."""
+    return _rope("sparstar_rope_fwd", x, table, start, positions, interleaved, out)
+
+
+def sparstar_rope_bwd(dy: torch.Tensor, table: torch.Tensor, start: int = 0, *, positions: torch.Tensor | None = None,
+                      interleaved: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient of sparstar_rope_fwd's x from the one of its result; `out` may be a slice of
+    the fused projection's gradient."""
+    return _rope("sparstar_rope_bwd", dy, table, start, positions, interleaved, out)
+
+
+# --------------------------------------------------------------------------
+# the paged 4-bit cache
+# --------------------------------------------------------------------------
+class PagedCache(NamedTuple):
+    """Pages of keys and values in 4 bits: two e2m1 codes per byte and one scale byte e + 127
+    per token, head and 32 channels; a value is code * 2^e.  Which pages are a sequence's, in
+    order, says an int32 tensor [B, n_table] beside it."""
+    k: torch.Tensor        # [n_pages, H, block_size, D / 2] uint8
+    v: torch.Tensor
+    k_scale: torch.Tensor  # [n_pages, H, block_size, D / 32] uint8
+    v_scale: torch.Tensor
+
+    @property
+    def block_size(self) -> int:
+        return self.k.shape[2]
+
+    @classmethod
+    def empty(cls, n_pages: int, H: int, D: int, block_size: int, device="cuda") -> "PagedCache":
+        """Pages without contents, which need no initialisation."""
+        def pool(n):
+            return torch.empty((n_pages, H, block_size, n), dtype=torch.uint8, device=device)
+
+        return cls(pool(D // 2), pool(D // 2), pool(D // 32), pool(D // 32))
+
+
+def _paged(c: PagedCache, pages: torch.Tensor, B: int, H: int, D: int, device: torch.device):
+    """(pages, n_table, n_pages) and the four pointers of a cache that fits B, H and D."""
+    if c.k.dim() != 4 or pages.dim() != 2:
+        raise ValueError("the cache's k must be [n_pages, H, block_size, D / 2], pages [B, n_table]")
+    n, u8, b = c.k.shape[0], torch.uint8, c.k.shape[2]
+    codes, scale = (n, H, b, D // 2), (n, H, b, D // 32)
+    ptrs = (_like(c.k, codes, u8, "cache.k", device), _like(c.v, codes, u8, "cache.v", device),
+            _like(c.k_scale, scale, u8, "cache.k_scale", device), _like(c.v_scale, scale, u8, "cache.v_scale", device))
+    table = _like(pages, (B, pages.shape[1]), torch.int32, "pages", device)
+    return (table, pages.shape[1], n), ptrs
+
+
+def sparstar_paged_write(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, pages: torch.Tensor, start: int = 0, *,
+                         starts: torch.Tensor | None = None, counts: torch.Tensor | None = None,
+                         table: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+                         interleaved: bool = False) -> None:
+    """Appends k and v [B, H, L, D] (strided as for sparstar_rope_fwd) to the sequences' pages at
+    row `start`, or at row starts[b] of each; counts[b] limits how many of a sequence's tokens
+    are written.  With a table, k is turned on the way by the position of each token: its row in
+    the cache, or positions[b, i]."""
+    ks, dev = _strided(k, "k"), k.device
+    vs = _strided(v, "v", dev, k.shape)
+    B, H, L, D = k.shape
+    where, ptrs = _paged(cache, pages, B, H, D, dev)
+    sp, cp = _like(starts, (B,), torch.int32, "starts", dev), _like(counts, (B,), torch.int32, "counts", dev)
+    pp = _like(positions, (B, L), torch.int32, "positions", dev)
+    turn = _table(table, dev) if table is not None else (None, 0, 0)
+    _launch("sparstar_paged_write", dev, k.data_ptr(), ks, v.data_ptr(), vs, B, H, L, D, cache.block_size, start, sp, cp,
+            *turn, int(interleaved), pp, *where, *ptrs)
+
+
+def sparstar_paged_read(cache: PagedCache, pages: torch.Tensor, start: int, L: int, *, want=("k", "v"), out=None):
+    """Rows [start, start + L) of every sequence in bf16, exactly: (k, v), each [B, H, L, D], or
+    None for one that `want` leaves out."""
+    if cache.k.dim() != 4 or not cache.k.is_cuda or pages.dim() != 2:
+        raise ValueError("the cache's k must be [n_pages, H, block_size, D / 2], on the GPU, pages [B, n_table]")
+    B, H, D, dev, bf16 = pages.shape[0], cache.k.shape[1], 2 * cache.k.shape[3], cache.k.device, torch.bfloat16
+    where, ptrs = _paged(cache, pages, B, H, D, dev)
+    shape = (B, H, L, D)
+    if out is None:
+        out = [torch.empty(shape, dtype=bf16, device=dev) if n in want else None for n in ("k", "v")]
+    kp, vp = _like(out[0], shape, bf16, "k", dev), _like(out[1], shape, bf16, "v", dev)
+    _launch("sparstar_paged_read", dev, *ptrs, B, H, start, L, D, cache.block_size, *where, kp, vp)
+    return tuple(out)
+
+
+@functools.lru_cache(maxsize=1024)
+def sparstar_paged_attn_workspace_bytes(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int) -> int:
+    return int(load().sparstar_paged_attn_workspace_bytes(B, H, Lq, Lk, D, block_size))
+
+
+@functools.lru_cache(maxsize=1024)
+def _paged_scratch(B: int, H: int, Lq: int, Lk: int, D: int, block_size: int, kv_stride: int) -> int:
+    """Bytes of workspace that a call makes use of (kv_stride 0: the dense one)."""
+    if load().sparstar_internal_paged_ranges(B, H, Lq, Lk, D, block_size, kv_stride) <= 1:
+        return 0
+    return sparstar_paged_attn_workspace_bytes(B, H, Lq, Lk, D, block_size)
+
+
+def _paged_attn(fn, q, cache, pages, lists, Lk, softmax_scale, lens, out, lse, return_lse, split, workspace):
+    B, H, Lq, D = _bhld(q, "q")
+    dev = q.device
+    where, ptrs = _paged(cache, pages, B, H, D, dev)
+    b = cache.block_size
+    Lk = where[1] * b if Lk is None else Lk
+    lp = _like(lens, (B,), torch.int32, "lens", dev)
+    listed = _lists(*lists, B, H, Lq, b, dev) if lists is not None else ()
+    o = torch.empty_like(q) if out is None else out
+    if lse is None and return_lse:
+        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=dev)
+    op, lsep = _like(o, q.shape, torch.bfloat16, "out", dev), _like(lse, (B, H, Lq), torch.float32, "lse", dev)
+    wp, wn = None, 0
+    if split:
+        if workspace is None:
+            need = _paged_scratch(B, H, Lq, Lk, D, b, listed[2] if listed else 0)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        if workspace is not None:
+            wp, wn = _scratch(workspace, dev)
+    _launch(fn, dev, q.data_ptr(), *ptrs, B, H, Lq, Lk, D, b, *where, lp, *listed, float(softmax_scale), op, lsep, wp, wn)
+    return o, lse
+
+
+def sparstar_paged_sparse_attn_fwd(q, cache: PagedCache, pages, kv_num_blocks, kv_indices, Lk: int | None = None,
+                                   softmax_scale: float = 0.0, *, lens: torch.Tensor | None = None,
+                                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                                   return_lse: bool = True, split: bool = True,
+                                   workspace: torch.Tensor | None = None):
+    """Block-sparse forward over the first Lk rows of the sequences' pages (all by default), or
+    the first lens[b] of each: returns (O, lse).  Block j of a sequence is its page j.
+    split=False runs a single pass without a workspace."""
+    return _paged_attn("sparstar_paged_sparse_attn_fwd", q, cache, pages, (kv_num_blocks, kv_indices), Lk,
+                       softmax_scale, lens, out, lse, return_lse, split, workspace)
+
+
+def sparstar_paged_dense_attn_fwd(q, cache: PagedCache, pages, Lk: int | None = None, softmax_scale: float = 0.0, *,
+                                  lens: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                                  lse: torch.Tensor | None = None, return_lse: bool = True, split: bool = True,
+                                  workspace: torch.Tensor | None = None):
+    """Dense forward over the sequences' pages: returns (O, lse)."""
+    return _paged_attn("sparstar_paged_dense_attn_fwd", q, cache, pages, None, Lk, softmax_scale, lens, out, lse,
+                       return_lse, split, workspace)
