@@ -1,6 +1,5 @@
 // Attention over the paged 4-bit key/value cache (paged.hip), dense or over block lists.
-#include "attn_device.h"
-#include "paged.h"
+#include "cache_attn_kernel.h"
 
 namespace sparstar {
 
@@ -83,6 +82,10 @@ __global__ __launch_bounds__(64) void paged_row_kernel(PagedAttnArgs a) {
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int d, int waves, bool dense, hipStream_t stream) {
   const int64_t rows = (int64_t)a.bh * a.lq;
+  if (waves > 1) {
+    if (d == 128) return dense ? launch_rows<128, true, Codes4>(a, waves, stream) : launch_rows<128, false, Codes4>(a, waves, stream);
+    return dense ? launch_rows<64, true, Codes4>(a, waves, stream) : launch_rows<64, false, Codes4>(a, waves, stream);
+  }
   if (d == 128 && dense) paged_row_kernel<128, true><<<rows, 64, 0, stream>>>(a);
   else if (d == 128) paged_row_kernel<128, false><<<rows, 64, 0, stream>>>(a);
   else if (dense) paged_row_kernel<64, true><<<rows, 64, 0, stream>>>(a);
