@@ -3,94 +3,380 @@
 
 namespace sparstar {
 
-// One wave per query row: 64 keys at a time, a key per lane for the scores, a pair of
-// channels per lane (D = 64: a channel) for the sum.
-template <int D, bool DENSE>
-__global__ __launch_bounds__(64) void paged_row_kernel(PagedAttnArgs a) {
-  __shared__ float qs[D];
-  constexpr int CPL = D / 64;  // channels per lane
-  const int lane = threadIdx.x;
-  const int64_t at = blockIdx.x, bh = at / a.lq, row = at - bh * a.lq, b = bh / a.heads, h = bh - b * a.heads;
-  for (int d = lane; d < D; d += 64) qs[d] = bf16_lo(a.q[at * D + d]);
-  __syncthreads();
+// A raw buffer of `n` bytes whose base is uniform.
+__device__ __forceinline__ uint32_t scale_byte(__amdgpu_buffer_rsrc_t rs, int at) {
+  return __builtin_amdgcn_raw_buffer_load_b8(rs, at, 0, 0);
+}
+
+// ---- up to 32 query rows: one work-group of W waves per (head, range of the list); each wave
+// has a share of the range's 64-key tiles and no barrier until the waves join what they found.
+//
+// On v_mfma_f32_16x16x32_bf16 (lane l, j = l / 16: A[m][k] m = l % 16, B[k][n] n = l % 16, k =
+// 8 j + i of the lane's eight; C[m][n] n = l % 16, m = 4 j + a):
+//   * S^T = K Q^T, 16 keys a product.  A lane loads the D / 4 channels G j .. of key l % 16
+//     straight into registers (16 rows: 1 KB in a row) and decodes them eight at a time; Q's
+//     operand takes the same order of channels;
+//   * softmax in the log2 domain against a running max that is only refreshed when some
+//     lane's sum of a tile's P exceeds 2^8;
+//   * O^T += V^T P^T, 32 keys a product: P is in S's layout, keys 16 (i / 4) + 4 j + i % 4, and
+//     V's operand comes in that order from LDS: a lane loads 32 channels of a key, decodes
+//     them and stores them as bf16 rows, which the transpose read takes by columns.  A product
+//     with ones sums the rounded P.
+template <int D, int NC, bool DENSE, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(D * NC > 128 ? 1 : 2, 2)))
+void paged_token_kernel(PagedAttnArgs a) {
+  constexpr int KS = D / 32;           // k-steps of S
+  constexpr int DT = D / 16;           // 16-channel tiles of O^T
+  constexpr int KW = D / 32;           // dwords of K codes per lane and 16 keys
+  constexpr int LPK = D / 32;          // lanes per key of a V load
+  constexpr int VL = LPK;              // V loads per tile: 64 / LPK keys each
+  constexpr int RB = 2 * D;            // bytes of a bf16 row
+  constexpr int VT = 64 * RB;
+  static_assert(VT >= DT * NC * 64 * 16, "a wave's sums fit its tile");
+  __shared__ __attribute__((aligned(1024))) uint8_t tiles[W][VT];
+  __shared__ float meta[W][3][16 * NC];
+  const int64_t bh = blockIdx.x / a.ranges;
+  const int range = (int)(blockIdx.x - bh * a.ranges);
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int l16 = lane % 16, j = lane / 16;
+  const int64_t b = bh / a.heads, h = bh - b * a.heads;
+
   int64_t len = a.lk;
   if (a.lens != nullptr) {
     const int n = a.lens[b];
     len = n < 0 ? 0 : (n < a.lk ? n : a.lk);
   }
   const int n_blk = (int)((len + a.block - 1) / a.block);
-  int n = n_blk;
+
+  // Q[n][(D / 4) j + 8 s + i]
+  bf16x8 qf[NC][KS];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int64_t row = 16 * c + l16;
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (row < a.lq) u = *reinterpret_cast<const uint4*>(a.q + (bh * a.lq + row) * D + D / 4 * j + 8 * s);
+      qf[c][s] = __builtin_bit_cast(bf16x8, u);
+    }
+
+  // The wave's 64-key tiles [first, end) of the list's (of all) blocks.
+  const int sub_bits = a.block == 128 ? 1 : 0;
+  int first, end;
   const int32_t* list = nullptr;
-  if constexpr (!DENSE) {
-    const int64_t r = bh * a.n_q + row / a.block;
-    n = a.kv_num_blocks[r];
-    n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
-    list = a.kv_indices + r * a.stride;
+  {
+    int n = n_blk;
+    if constexpr (!DENSE) {
+      n = a.kv_num_blocks[bh];  // (one query block)
+      n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
+      list = a.kv_indices + bh * a.stride;
+    }
+    const int part = range * W + wave, parts = a.ranges * W;
+    first = __builtin_amdgcn_readfirstlane((int)(((int64_t)n << sub_bits) * part / parts));
+    end = __builtin_amdgcn_readfirstlane((int)(((int64_t)n << sub_bits) * (part + 1) / parts));
   }
-  float m = -INFINITY, l = 0.f, le = 0.f, o[CPL] = {};
-  for (int e = 0; e < n; ++e) {
-    const int j = DENSE ? e : list[e];
-    if (j < 0 || j >= n_blk) continue;
-    const int64_t page = a.pages[b * a.n_table + j];
-    if (page < 0 || page >= a.n_pages) continue;
-    for (int sub = 0; sub < a.block; sub += 64) {
-      const int64_t left = len - ((int64_t)j * a.block + sub);
-      if (left <= 0) break;
-      const int64_t r0 = (page * a.heads + h) * a.block + sub;
-      float s = -INFINITY;
-      if (lane < left) {
-        s = 0.f;
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(a.k_cache + (r0 + lane) * (D / 2));
-        for (int c = 0; c < D / 8; ++c) {
-          const float sc = __uint_as_float((uint32_t)a.k_scale[(r0 + lane) * (D / 32) + c / 4] << 23);
-          const auto u0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[c], sc, 0);
-          const auto u1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[c], sc, 1);
-          const auto u2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[c], sc, 2);
-          const auto u3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[c], sc, 3);
-          const float* q = qs + 8 * c;
-          s += u0[0] * q[0] + u0[1] * q[1] + u1[0] * q[2] + u1[1] * q[3];
-          s += u2[0] * q[4] + u2[1] * q[5] + u3[0] * q[6] + u3[1] * q[7];
-        }
-        s *= a.scale_log2;
+  // Entries 64 at a time in VGPRs: the block and its page; -1 where there is none.
+  int breg = -1, preg = 0, lbase = 0;
+  auto load_batch = [&](int base) {
+    lbase = base;
+    int e = -1;
+    if ((base + lane) << sub_bits < end) e = DENSE ? base + lane : list[base + lane];
+    if (e < 0 || e >= n_blk) e = -1;
+    preg = e < 0 ? -1 : a.pages[b * a.n_table + e];
+    if (preg < 0 || preg >= a.n_pages) e = -1, preg = 0;
+    breg = e;
+    asm volatile("; list batch %0 %1" ::"v"(breg), "v"(preg));
+  };
+  struct Tile {
+    int left;     // keys, <= 0: none
+    int64_t row;  // of the pool
+  };
+  auto fetch = [&](int i) -> Tile {
+    if (i >= end) return Tile{0, 0};
+    const int e = i >> sub_bits, sub = i & ((1 << sub_bits) - 1);
+    if (e >= lbase + 64) load_batch(lbase + 64);
+    const int blk = __builtin_amdgcn_readlane(breg, e - lbase), page = __builtin_amdgcn_readlane(preg, e - lbase);
+    const int64_t left = blk < 0 ? 0 : len - ((int64_t)blk * a.block + 64 * sub);
+    return Tile{(int)(left < 0 ? 0 : (left > 64 ? 64 : left)), ((int64_t)page * a.heads + h) * a.block + 64 * sub};
+  };
+
+  struct Raw {
+    uint32_t k[4][KW], ks[4];  // by 16 keys
+    uint4 v[VL];
+    uint32_t vs[VL];
+  };
+  const int kat = l16 * (D / 2) + j * (D / 8), ksat = l16 * (D / 32) + j * (D / 32) / 4;
+  auto load = [&](Tile t, Raw& r) {
+    const uint32_t n = (uint32_t)t.left;
+    const auto kr = tile_rsrc(a.k_cache + t.row * (D / 2), n * (D / 2)), vr = tile_rsrc(a.v_cache + t.row * (D / 2), n * (D / 2));
+    const auto ksr = tile_rsrc(a.k_scale + t.row * (D / 32), n * (D / 32));
+    const auto vsr = tile_rsrc(a.v_scale + t.row * (D / 32), n * (D / 32));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if constexpr (D == 128) {
+        const uint4 w = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kr, kat + 1024 * u, 0, 0));
+        r.k[u][0] = w.x, r.k[u][1] = w.y, r.k[u][2] = w.z, r.k[u][3] = w.w;
+      } else {
+        const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(kr, kat + 512 * u, 0, 0));
+        r.k[u][0] = w.x, r.k[u][1] = w.y;
       }
-      float mx = s;
-      for (int i = 32; i > 0; i /= 2) mx = fmaxf(mx, __shfl_xor(mx, i));
-      const float mn = fmaxf(m, mx), alpha = mn == -INFINITY ? 0.f : exp2f(m - mn);
-      const float p = mn == -INFINITY ? 0.f : exp2f(s - mn);
-      m = mn;
-      l = l * alpha + p;
-      for (int i = 0; i < CPL; ++i) o[i] *= alpha;
-      const int keys = left < 64 ? (int)left : 64;
-      for (int k = 0; k < keys; ++k) {
-        const float pk = __shfl(p, k);
-        const uint8_t* w = a.v_cache + (r0 + k) * (D / 2);
-        for (int i = 0; i < CPL; ++i) {
-          const int d = CPL * lane + i;
-          const float sc = __uint_as_float((uint32_t)a.v_scale[(r0 + k) * (D / 32) + d / 32] << 23);
-          const auto u = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)w[d / 2], sc, 0);
-          o[i] = fmaf(pk, d % 2 ? u[1] : u[0], o[i]);
+      r.ks[u] = scale_byte(ksr, ksat + 16 * (D / 32) * u);
+    }
+#pragma unroll
+    for (int u = 0; u < VL; ++u) {
+      r.v[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(vr, 16 * lane + 1024 * u, 0, 0));
+      r.vs[u] = scale_byte(vsr, lane + 64 * u);
+    }
+  };
+
+  // V in LDS: the chunks of row r are permuted so that eight consecutive rows' pairs of chunks
+  // (the transpose read) and two rows' chunks four apart (the stores) fall on different banks.
+  auto swz = [](int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
+  uint8_t* const vt = tiles[wave];
+  const int vrow = lane / LPK, vc = 4 * (lane % LPK);
+  uint32_t vput[4], vget[DT];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) vput[i] = (uint32_t)(vrow * RB + 16 * ((vc + i) ^ swz(vrow)));
+  {
+    const int r = 4 * j + (lane & 15) / 4, p = lane & 3;  // rows 4 j .. + 3, four pieces of 8 bytes
+#pragma unroll
+    for (int t = 0; t < DT; ++t) vget[t] = (uint32_t)(r * RB + 16 * ((2 * t + p / 2) ^ swz(r)) + 8 * (p % 2));
+  }
+  auto read_v = [&](int t, int half) -> bf16x8 {
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(vt + vget[t] + 32 * half * RB);
+    const s16x4 lo = lds_read_tr(p), hi = lds_read_tr(p + 16 * D);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  f32x4 acc[DT][NC], accl[NC];
+  float m_run[NC], le_run[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    accl[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run[c] = -INFINITY, le_run[c] = 0.f;
+  }
+  const uint32_t one2 = 0x3f803f80u;
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, make_uint4(one2, one2, one2, one2));
+
+  auto step = [&](Tile cur, const Raw& r) {
+    f32x4 s[4][NC];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float sc = __uint_as_float(r.ks[u] << 23);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s[u][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const bf16x8 kv = decode8_4bit(r.k[u][k], sc);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qf[c][k], s[u][c], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < VL; ++u) {
+      const float sc = __uint_as_float(r.vs[u] << 23);
+      const uint32_t w[4] = {r.v[u].x, r.v[u].y, r.v[u].z, r.v[u].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<bf16x8*>(vt + vput[i] + u * (64 / LPK) * RB) = decode8_4bit(w[i], sc);
+    }
+    if (cur.left < 64) {
+      asm volatile("; mask");
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * u + 4 * j + e >= cur.left)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) s[u][c][e] = -INFINITY;
+    }
+    bf16x8 pk[2][NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float p[16], se = 0.f;
+      const float neg_m = m_run[c] == -INFINITY ? INFINITY : -m_run[c];  // (no key seen yet: takes the exact path)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(s[e / 4][c][e % 4], a.scale_log2, neg_m));
+        se += p[e];
+      }
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(se <= 256.f)) != 0, 0)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e / 4][c][e % 4]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.scale_log2;
+        const float mn = fmaxf(m_run[c], mx), alpha = mn == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[c] - mn);
+        m_run[c] = mn;
+        le_run[c] *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) accl[c][e] *= alpha;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][c][e] *= alpha;
+        const float off = mn == -INFINITY ? 0.f : -mn;
+        se = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(s[e / 4][c][e % 4], a.scale_log2, off));
+          se += p[e];
         }
+      }
+      le_run[c] += se;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const float* x = p + 8 * half;
+        pk[half][c] = __builtin_bit_cast(
+            bf16x8, make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]), pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7])));
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) accl[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pk[half][c], accl[c], 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const bf16x8 v = read_v(t, half);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pk[half][c], acc[t][c], 0, 0, 0);
+      }
+    }
+  };
+
+  if (first < end) {
+    load_batch(first >> sub_bits);
+    Raw r0, r1;
+    Tile t0 = fetch(first), t1 = fetch(first + 1);
+    load(t0, r0);
+    load(t1, r1);
+    for (int i = first; i < end; i += 2) {
+      step(t0, r0);
+      t0 = fetch(i + 2);
+      load(t0, r0);
+      if (i + 1 >= end) break;
+      step(t1, r1);
+      t1 = fetch(i + 3);
+      load(t1, r1);
+    }
+  }
+
+  // The waves join: with M = max_w m_w, sums of 2^(m_w - M) times each one's, every wave for some
+  // of the tiles of O^T.
+  float4* const mine = reinterpret_cast<float4*>(vt) + lane;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) mine[64 * (t * NC + c)] = make_float4(acc[t][c][0], acc[t][c][1], acc[t][c][2], acc[t][c][3]);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    float le = le_run[c];
+    le += __shfl_xor(le, 16);
+    le += __shfl_xor(le, 32);
+    if (j == 0) meta[wave][0][16 * c + l16] = m_run[c], meta[wave][1][16 * c + l16] = accl[c][0], meta[wave][2][16 * c + l16] = le;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int64_t row = 16 * c + l16;
+    float m = -INFINITY, l = 0.f, le = 0.f, f[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, meta[w][0][16 * c + l16]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      // (a wave that saw no key has m = -inf and sums of zero, a NaN among its sums passes on)
+      const float x = meta[w][0][16 * c + l16];
+      f[w] = x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x - m);
+      l = fmaf(meta[w][1][16 * c + l16], f[w], l);
+      le = fmaf(meta[w][2][16 * c + l16], f[w], le);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t at = bh * a.lq + row, prow = (int64_t)range * a.bh * a.lq + at;
+    if (wave == 0 && j == 0 && row < a.lq) {
+      if (a.ranges > 1) reinterpret_cast<float4*>(a.part_meta)[prow] = make_float4(m, l, le, 0.f);
+      else if (a.lse != nullptr) a.lse[at] = le == 0.f ? -INFINITY : (m + log2f(le)) * 0.69314718055994530942f;
+    }
+#pragma unroll
+    for (int t = wave; t < DT; t += W) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float4 u = reinterpret_cast<const float4*>(tiles[w])[64 * (t * NC + c) + lane];
+        x.x = fmaf(u.x, f[w], x.x), x.y = fmaf(u.y, f[w], x.y), x.z = fmaf(u.z, f[w], x.z), x.w = fmaf(u.w, f[w], x.w);
+      }
+      if (row >= a.lq) continue;
+      if (a.ranges > 1) {
+        *reinterpret_cast<float4*>(a.part32 + prow * D + 16 * t + 4 * j) = x;
+      } else {
+        *reinterpret_cast<uint2*>(a.o + at * D + 16 * t + 4 * j) =
+            make_uint2(pack2_bf16(x.x * inv, x.y * inv), pack2_bf16(x.z * inv, x.w * inv));
       }
     }
   }
-  for (int i = 32; i > 0; i /= 2) l += __shfl_xor(l, i);
+}
+
+// Joins the ranges of a row, D / 4 threads and G groups of them, each over every G-th range.
+template <int D, int G>
+__global__ __launch_bounds__(D / 4 * G) void paged_join_kernel(PagedAttnArgs a) {
+  constexpr int LPR = D / 4;
+  __shared__ float4 red[G][LPR];
+  __shared__ float meta[G][3];
+  const int c = threadIdx.x % LPR, g = threadIdx.x / LPR;
+  const int64_t rows = (int64_t)a.bh * a.lq, row = blockIdx.x;
+  float m = -INFINITY, l = 0.f, le = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int r = g; r < a.ranges; r += G) {
+    const int64_t p = (int64_t)r * rows + row;
+    const float4 y = reinterpret_cast<const float4*>(a.part_meta)[p];
+    const float4 u = *reinterpret_cast<const float4*>(a.part32 + p * D + 4 * c);
+    if (y.y == 0.f) continue;  // no key seen; NaN passes on
+    const float mn = fmaxf(m, y.x), s = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    const float t = y.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(y.x - mn);
+    l = fmaf(l, s, y.y * t), le = fmaf(le, s, y.z * t);
+    x.x = fmaf(u.x, t, x.x * s), x.y = fmaf(u.y, t, x.y * s), x.z = fmaf(u.z, t, x.z * s), x.w = fmaf(u.w, t, x.w * s);
+    m = mn;
+  }
+  red[g][c] = x;
+  if (c == 0) meta[g][0] = m, meta[g][1] = l, meta[g][2] = le;
+  __syncthreads();
+  if (g != 0) return;
+  float mm = m;
+#pragma unroll
+  for (int i = 1; i < G; ++i) mm = fmaxf(mm, meta[i][0]);
+  // (a group without keys has m = -inf and sums of zero, or NaN, which passes on)
+  auto weight = [&](float v) { return v == -INFINITY ? (mm == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(v - mm); };
+  float s = weight(m);
+  l *= s, le *= s, x.x *= s, x.y *= s, x.z *= s, x.w *= s;
+#pragma unroll
+  for (int i = 1; i < G; ++i) {
+    s = weight(meta[i][0]);
+    const float4 u = red[i][c];
+    l = fmaf(meta[i][1], s, l), le = fmaf(meta[i][2], s, le);
+    x.x = fmaf(u.x, s, x.x), x.y = fmaf(u.y, s, x.y), x.z = fmaf(u.z, s, x.z), x.w = fmaf(u.w, s, x.w);
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int i = 0; i < CPL; ++i)
-    a.o[at * D + CPL * lane + i] = (uint16_t)pack2_bf16(o[i] * inv, 0.f);
-  if (a.lse != nullptr && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+  *reinterpret_cast<uint2*>(a.o + row * D + 4 * c) =
+      make_uint2(pack2_bf16(x.x * inv, x.y * inv), pack2_bf16(x.z * inv, x.w * inv));
+  if (a.lse != nullptr && c == 0) a.lse[row] = le == 0.f ? -INFINITY : (mm + log2f(le)) * 0.69314718055994530942f;
+}
+
+template <int D, bool DENSE>
+static hipError_t launch_mode(const PagedAttnArgs& a, int waves, hipStream_t stream) {
+  if (waves > 1) return launch_rows<D, DENSE, Codes4>(a, waves, stream);
+  const int64_t groups = (int64_t)a.bh * a.ranges;
+  constexpr int W = kTokenWaves;
+  if (a.lq <= 16) paged_token_kernel<D, 1, DENSE, W><<<groups, 64 * W, 0, stream>>>(a);
+  else paged_token_kernel<D, 2, DENSE, W><<<groups, 64 * W, 0, stream>>>(a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.ranges == 1) return e;
+  paged_join_kernel<D, 4><<<(int64_t)a.bh * a.lq, D / 4 * 4, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, int d, int waves, bool dense, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.bh * a.lq;
-  if (waves > 1) {
-    if (d == 128) return dense ? launch_rows<128, true, Codes4>(a, waves, stream) : launch_rows<128, false, Codes4>(a, waves, stream);
-    return dense ? launch_rows<64, true, Codes4>(a, waves, stream) : launch_rows<64, false, Codes4>(a, waves, stream);
-  }
-  if (d == 128 && dense) paged_row_kernel<128, true><<<rows, 64, 0, stream>>>(a);
-  else if (d == 128) paged_row_kernel<128, false><<<rows, 64, 0, stream>>>(a);
-  else if (dense) paged_row_kernel<64, true><<<rows, 64, 0, stream>>>(a);
-  else paged_row_kernel<64, false><<<rows, 64, 0, stream>>>(a);
-  return hipGetLastError();
+  if (d == 128) return dense ? launch_mode<128, true>(a, waves, stream) : launch_mode<128, false>(a, waves, stream);
+  return dense ? launch_mode<64, true>(a, waves, stream) : launch_mode<64, false>(a, waves, stream);
 }
 
 }  // namespace sparstar
