@@ -15,7 +15,7 @@ struct RopeTableArgs {
   int64_t rows;
   int axes, pairs;
   double amplitude;
-  double turns[kRopeMaxPairs];  // freq / (2 pi)
+  double quarters[kRopeMaxPairs];  // freq 2 / pi: quarter turns per step
   uint8_t axis[kRopeMaxPairs];
 };
 

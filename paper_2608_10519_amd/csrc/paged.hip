@@ -10,107 +10,167 @@
 
 namespace sparstar {
 
-// One thread per (K or V, token, chunk of 8 channels, group of heads); four neighbouring
-// threads share a scale.
-template <bool INTERLEAVED>
-__global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a, int groups, int per_group) {
-  const int cpr = a.d / 8;
-  const int64_t i = group_of_rows() * 256 + threadIdx.x;
-  const int64_t tokens = (int64_t)a.b * a.l, w = i / cpr;
-  if (w >= 2 * tokens * groups) return;  // (whole rows of cpr threads: whole groups of four)
-  const int c = (int)(i - w * cpr);
-  const int g2 = (int)(w / tokens), is_v = g2 >= groups, g = is_v ? g2 - groups : g2;
-  const int64_t at = w - g2 * tokens, b = at / a.l, l = at - b * a.l;
-  const int64_t row = (a.starts != nullptr ? a.starts[b] : a.start) + l;
+// The largest magnitude of a group of four threads' values, as bf16 bits, by each of them.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t group_max(uint32_t m) {
+  m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xb1, 15, 15, true));  // lanes 1 0 3 2
+  return max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4e, 15, 15, true));  // lanes 2 3 0 1
+}
+
+// Scale byte of the 32 channels that this thread and its three neighbours hold.
+__device__ __forceinline__ uint32_t scale_byte_of(uint4 w) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  u16x2 big = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, u[i] & 0x7fff7fffu));
+  uint32_t m = group_max(max(big[0], big[1]));
+  bool nan = false;
+  if (m >= 0x7f80) {  // not finite (the same in all four): the largest of what is
+    uint32_t top = 0;
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t x = (i % 2 ? u[i / 2] >> 16 : u[i / 2]) & 0x7fff;
+      top = max(top, x);
+      if (x < 0x7f80) m = max(m, x);
+    }
+    nan = group_max(top) > 0x7f80;
+    m = group_max(m);
+  }
+  // m = 1.f 2^(E - 127) with E and the 7 bits f its fields: e is E - 127 - 2, and one more where
+  // 1.f > 3/2, 6 being 3/2 2^2
+  const int byte = (int)((m + 63) >> 7) - 2;
+  return nan ? kPagedNan : (uint32_t)min(max(byte, kPagedExpMin + 127), kPagedExpMax + 127);
+}
+
+// One thread per (K or V, token, chunk of 8 channels) and N heads, as rope_kernel; four
+// neighbouring threads share a scale.
+template <bool INTERLEAVED, int N>
+__global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a) {
+  const TokenChunk t = token_chunk((int64_t)a.b * a.l, a.l, a.d == 128 ? 4 : 3);
+  if (!t.ok) return;  // (whole rows of threads: whole groups of four)
+  // (K and V in turn: the turns' work lies beside V's loads)
+  const bool is_v = t.group % 2 != 0;
+  const int h0 = (int)(t.group / 2) * N, left = a.heads - h0, c = t.c;
+  const int64_t row = (a.starts != nullptr ? a.starts[t.b] : a.start) + t.l;
+  const int block_bits = a.block == 128 ? 7 : 6;
   // rows outside the table do not exist: the tokens that would go there are dropped
-  if (row < 0 || row >= a.n_table * a.block) return;
-  if (a.counts != nullptr && l >= a.counts[b]) return;
-  const int64_t page = a.pages[b * a.n_table + row / a.block];
+  if (row < 0 || row >= a.n_table << block_bits) return;
+  if (a.counts != nullptr && t.l >= a.counts[t.b]) return;
+  const int64_t page = a.pages[t.b * a.n_table + (row >> block_bits)];
   if (page < 0 || page >= a.n_pages) return;
   ChunkTurn u;
   u.other = -1;
-  if (!is_v) u = chunk_turn(a.turn, a.turn.table != nullptr ? table_row(a.turn, at, row) : 0, c);
+  if (!is_v && a.turn.table != nullptr) u = chunk_turn(a.turn, table_row(a.turn, t.at, row), c);
   const Strides& s = is_v ? a.vs : a.ks;
-  const uint16_t* x = (is_v ? a.v : a.k) + b * s.b + l * s.l;
-  uint8_t* const codes = is_v ? a.v_pages : a.k_pages;
-  uint8_t* const scale = is_v ? a.v_scale : a.k_scale;
-  const int end = (g + 1) * per_group < a.heads ? (g + 1) * per_group : a.heads;
-  for (int h = g * per_group; h < end; ++h) {
-    const uint16_t* p = x + h * s.h;
-    uint4 own = *reinterpret_cast<const uint4*>(p + 8 * c);
-    if (u.other >= 0) {
-      const uint4 other = INTERLEAVED ? own : *reinterpret_cast<const uint4*>(p + u.other);
-      own = turned(u, own, other, INTERLEAVED);
-    }
-    float y[8], amax = 0.f;
-    bool bad = false;
+  const uint16_t* x = (is_v ? a.v : a.k) + t.b * s.b + t.l * s.l + h0 * s.h;
+  const int64_t at_row = ((page * a.heads + h0) << block_bits) + (row & (a.block - 1));
+  uint8_t* const codes = (is_v ? a.v_pages : a.k_pages) + at_row * (a.d / 2) + 4 * c;
+  uint8_t* const scale = (is_v ? a.v_scale : a.k_scale) + at_row * (a.d / 32) + c / 4;
+  uint4 own[N], other[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = bf16_at(own, e);
-      const float m = fabsf(y[e]);
-      if (m < INFINITY) amax = fmaxf(amax, m);
-      bad |= y[e] != y[e];
-    }
-    amax = fmaxf(amax, __shfl_xor(amax, 1));
-    amax = fmaxf(amax, __shfl_xor(amax, 2));
-    const uint64_t any = __builtin_amdgcn_ballot_w64(bad) >> (threadIdx.x % 64 & ~3);
-    // amax = m 2^x with 1/2 <= m < 1, and 6 = 3/4 2^3
-    int e = kPagedExpMin;
-    if (amax > 0.f) {
-      e = __builtin_amdgcn_frexp_expf(amax) - (__builtin_amdgcn_frexp_mantf(amax) <= 0.75f ? 3 : 2);
-      e = e < kPagedExpMin ? kPagedExpMin : (e > kPagedExpMax ? kPagedExpMax : e);
-    }
-    const float inv = __builtin_amdgcn_ldexpf(1.f, -e);
-    // (the conversion rounds to the nearest, ties to even, and saturates)
+  for (int h = 0; h < N; ++h) {
+    if (h >= left) continue;
+    own[h] = *reinterpret_cast<const uint4*>(x + h * s.h + 8 * c);
+    if (!INTERLEAVED && u.other >= 0) other[h] = *reinterpret_cast<const uint4*>(x + h * s.h + u.other);
+  }
+#pragma unroll
+  for (int h = 0; h < N; ++h) {
+    if (h >= left) continue;
+    const uint4 w = u.other >= 0 ? turned(u, own[h], INTERLEAVED ? own[h] : other[h], INTERLEAVED) : own[h];
+    const uint32_t byte = scale_byte_of(w);
+    // (the conversion divides by the scale, rounds to the nearest, ties to even, and saturates)
+    const float sc = __uint_as_float(byte << 23);
     uint32_t r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[0] * inv, y[1] * inv, 1.f, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[2] * inv, y[3] * inv, 1.f, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[4] * inv, y[5] * inv, 1.f, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[6] * inv, y[7] * inv, 1.f, 3);
-    const int64_t at_row = (page * a.heads + h) * a.block + row % a.block;
-    *reinterpret_cast<uint32_t*>(codes + at_row * (a.d / 2) + 4 * c) = r;
-    if (c % 4 == 0) scale[at_row * (a.d / 32) + c / 4] = (uint8_t)((any & 15) != 0 ? kPagedNan : e + 127);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.x), sc, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.y), sc, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.z), sc, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.w), sc, 3);
+    *reinterpret_cast<uint32_t*>(codes + h * (a.block * (a.d / 2))) = r;
+    if (c % 4 == 0) scale[h * (a.block * (a.d / 32))] = (uint8_t)byte;
   }
 }
 
-// One thread per 8 codes.
+// One work-group per (K or V, batch * head, P times 256 / TPR rows), TPR threads a row with W
+// times 8 channels each.
+template <int CPR, int W, int P, bool ONCE>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedArgs a) {
-  const int cpr = a.d / 8;
-  const int64_t per_b = (int64_t)a.heads * a.l * cpr, n = a.b * per_b;
-  int64_t i = group_of_rows() * 256 + threadIdx.x;
-  // the first n threads take K where it is wanted, the next n (or the first) V
-  const bool is_v = a.k_out == nullptr || i >= n;
-  if (a.k_out != nullptr && is_v) i -= n;
-  if (i >= n || (is_v && a.v_out == nullptr)) return;
-  const int64_t b = i / per_b, r = i - b * per_b, w = r / cpr, h = w / a.l, row = a.start + w - h * a.l;
-  const int c = (int)(r - w * cpr);
-  const int64_t page = a.pages[b * a.n_table + row / a.block];
-  uint4 out = make_uint4(0, 0, 0, 0);
-  if (page >= 0 && page < a.n_pages) {
-    const int64_t at_row = (page * a.heads + h) * a.block + row % a.block;
-    const uint32_t u = *reinterpret_cast<const uint32_t*>((is_v ? a.v_pages : a.k_pages) + at_row * (a.d / 2) + 4 * c);
-    const float sc = __uint_as_float((uint32_t)(is_v ? a.v_scale : a.k_scale)[at_row * (a.d / 32) + c / 4] << 23);
-    out.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 0));
-    out.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 1));
-    out.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 2));
-    out.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, sc, 3));
+  constexpr int TPR = CPR / W, RPP = 256 / TPR;
+  const int64_t per = (a.l + RPP * P - 1) / (RPP * P), n = (int64_t)a.b * a.heads * per, w0 = group_of_rows();
+  // the first n work-groups take K where it is wanted, the next n (or the first) V
+  const bool is_v = a.k_out == nullptr || w0 >= n;
+  const int64_t w = a.k_out != nullptr && is_v ? w0 - n : w0;
+  if (w >= n) return;
+  const int64_t bh = divide(w, per), b = divide(bh, a.heads), h = bh - b * a.heads;
+  const int64_t l0 = (w - bh * per) * (RPP * P) + threadIdx.x / TPR;
+  const int c = threadIdx.x % TPR, block_bits = a.block == 128 ? 7 : 6;
+  const uint8_t* const codes = is_v ? a.v_pages : a.k_pages;
+  const uint8_t* const scale = is_v ? a.v_scale : a.k_scale;
+  uint32_t u[P][W];
+  float sc[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+#pragma unroll
+    for (int k = 0; k < W; ++k) u[i][k] = 0;
+    sc[i] = 0.f;
+    const int64_t l = l0 + i * RPP, row = a.start + l;
+    if (l >= a.l) continue;
+    const int64_t page = a.pages[b * a.n_table + (row >> block_bits)];
+    if (page < 0 || page >= a.n_pages) continue;
+    const int64_t at_row = ((page * a.heads + h) << block_bits) + (row & (a.block - 1));
+    __builtin_memcpy(u[i], __builtin_assume_aligned(codes + at_row * (4 * CPR) + 4 * W * c, 4 * W), 4 * W);
+    sc[i] = __uint_as_float((uint32_t)scale[at_row * (CPR / 4) + W * c / 4] << 23);
   }
-  *reinterpret_cast<uint4*>((is_v ? a.v_out : a.k_out) + 8 * i) = out;
+  uint16_t* const out = (is_v ? a.v_out : a.k_out) + ((bh * a.l + l0) * TPR + c) * (8 * W);
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    if (l0 + i * RPP >= a.l) continue;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      uint4 r;
+      r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u[i][k], sc[i], 0));
+      r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u[i][k], sc[i], 1));
+      r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u[i][k], sc[i], 2));
+      r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u[i][k], sc[i], 3));
+      uint16_t* const to = out + i * (RPP * CPR * 8) + 8 * k;
+      if constexpr (ONCE) store_once(to, r);
+      else *reinterpret_cast<uint4*>(to) = r;
+    }
+  }
+}
+
+template <int N>
+static hipError_t launch_writes(const PagedArgs& a, hipStream_t stream) {
+  const dim3 grid = token_grid(2 * ((a.heads + N - 1) / N), (int64_t)a.b * a.l, a.d);
+  if (a.turn.interleaved) paged_write_kernel<true, N><<<grid, 256, 0, stream>>>(a);
+  else paged_write_kernel<false, N><<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_write(const PagedArgs& a, hipStream_t stream) {
-  const int per = 1, groups = (a.heads + per - 1) / per;
-  const int64_t threads = 2 * (int64_t)a.b * a.l * groups * (a.d / 8);
-  const dim3 grid = rows_of_groups((threads + 255) / 256);
-  if (a.turn.interleaved) paged_write_kernel<true><<<grid, 256, 0, stream>>>(a, groups, per);
-  else paged_write_kernel<false><<<grid, 256, 0, stream>>>(a, groups, per);
+  return (int64_t)a.b * a.heads * a.l >= 8192 ? launch_writes<3>(a, stream) : launch_writes<1>(a, stream);
+}
+
+template <int CPR, int W, int P, bool ONCE>
+static hipError_t launch_reads(const PagedArgs& a, hipStream_t stream) {
+  const int64_t rows = 256 / (CPR / W) * P, n = (int64_t)a.b * a.heads * ((a.l + rows - 1) / rows);
+  const dim3 grid = rows_of_groups(n * ((a.k_out != nullptr) + (a.v_out != nullptr)));
+  paged_read_kernel<CPR, W, P, ONCE><<<grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
+// Rows that the last-level cache holds, 256 MB, are best written past the L2 with 16 bytes a
+// lane side by side: 24 heads of 11,520 rows, D = 128, K and V (141 MB) 26 us, 37 with 32
+// bytes a lane through the L2; K alone 14.8 and 19.3.  Beyond it the latter is the faster:
+// 72,000 rows 216 and 263 us, K alone (442 MB) 110 and 132.
+template <int CPR>
+static hipError_t launch_reads(const PagedArgs& a, hipStream_t stream) {
+  const double bytes = 16.0 * CPR * a.b * a.heads * a.l * ((a.k_out != nullptr) + (a.v_out != nullptr));
+  return bytes <= 192e6 ? launch_reads<CPR, 1, 2, true>(a, stream) : launch_reads<CPR, 2, 1, false>(a, stream);
+}
+
 hipError_t launch_paged_read(const PagedArgs& a, hipStream_t stream) {
-  const int64_t n = (int64_t)a.b * a.heads * a.l * (a.d / 8) * ((a.k_out != nullptr) + (a.v_out != nullptr));
-  paged_read_kernel<<<rows_of_groups((n + 255) / 256), 256, 0, stream>>>(a);
-  return hipGetLastError();
+  return a.d == 128 ? launch_reads<16>(a, stream) : launch_reads<8>(a, stream);
 }
 
 }  // namespace sparstar

@@ -35,18 +35,19 @@ void paged_token_kernel(PagedAttnArgs a) {
   static_assert(VT >= DT * NC * 64 * 16, "a wave's sums fit its tile");
   __shared__ __attribute__((aligned(1024))) uint8_t tiles[W][VT];
   __shared__ float meta[W][3][16 * NC];
-  const int64_t bh = blockIdx.x / a.ranges;
-  const int range = (int)(blockIdx.x - bh * a.ranges);
+  const uint32_t head = blockIdx.x / (uint32_t)a.ranges;
+  const int range = (int)(blockIdx.x - head * (uint32_t)a.ranges);
+  const int64_t bh = head, b = head / (uint32_t)a.heads, h = head % (uint32_t)a.heads;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int l16 = lane % 16, j = lane / 16;
-  const int64_t b = bh / a.heads, h = bh - b * a.heads;
 
   int64_t len = a.lk;
   if (a.lens != nullptr) {
     const int n = a.lens[b];
     len = n < 0 ? 0 : (n < a.lk ? n : a.lk);
   }
-  const int n_blk = (int)((len + a.block - 1) / a.block);
+  const int sub_bits = a.block == 128 ? 1 : 0;
+  const int n_blk = (int)((len + a.block - 1) >> (6 + sub_bits));
 
   // Q[n][(D / 4) j + 8 s + i]
   bf16x8 qf[NC][KS];
@@ -61,7 +62,6 @@ void paged_token_kernel(PagedAttnArgs a) {
     }
 
   // The wave's 64-key tiles [first, end) of the list's (of all) blocks.
-  const int sub_bits = a.block == 128 ? 1 : 0;
   int first, end;
   const int32_t* list = nullptr;
   {
@@ -71,9 +71,10 @@ void paged_token_kernel(PagedAttnArgs a) {
       n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
       list = a.kv_indices + bh * a.stride;
     }
-    const int part = range * W + wave, parts = a.ranges * W;
-    first = __builtin_amdgcn_readfirstlane((int)(((int64_t)n << sub_bits) * part / parts));
-    end = __builtin_amdgcn_readfirstlane((int)(((int64_t)n << sub_bits) * (part + 1) / parts));
+    const uint32_t part = range * W + wave, parts = a.ranges * W, all = (uint32_t)n << sub_bits;
+    const uint32_t each = all / parts, more = all - each * parts;  // the first `more` parts take one more
+    first = __builtin_amdgcn_readfirstlane((int)(part * each + (part < more ? part : more)));
+    end = first + (int)each + (part < more ? 1 : 0);
   }
   // Entries 64 at a time in VGPRs: the block and its page; -1 where there is none.
   int breg = -1, preg = 0, lbase = 0;
@@ -251,16 +252,23 @@ void paged_token_kernel(PagedAttnArgs a) {
     Raw r0, r1;
     Tile t0 = fetch(first), t1 = fetch(first + 1);
     load(t0, r0);
+    __builtin_amdgcn_sched_barrier(0);  // (a tile's loads stay in the order of the tiles, which is that of the waits)
     load(t1, r1);
-    for (int i = first; i < end; i += 2) {
+    __builtin_amdgcn_sched_barrier(0);
+    int i = first;
+    for (; i + 1 < end; i += 2) {  // (no way out in between, which would make every wait one for all loads)
       step(t0, r0);
+      __builtin_amdgcn_sched_barrier(0);
       t0 = fetch(i + 2);
       load(t0, r0);
-      if (i + 1 >= end) break;
+      __builtin_amdgcn_sched_barrier(0);
       step(t1, r1);
+      __builtin_amdgcn_sched_barrier(0);
       t1 = fetch(i + 3);
       load(t1, r1);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    if (i < end) step(t0, r0);
   }
 
   // The waves join: with M = max_w m_w, sums of 2^(m_w - M) times each one's, every wave for some
@@ -327,6 +335,7 @@ __global__ __launch_bounds__(D / 4 * G) void paged_join_kernel(PagedAttnArgs a) 
   const int64_t rows = (int64_t)a.bh * a.lq, row = blockIdx.x;
   float m = -INFINITY, l = 0.f, le = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int r = g; r < a.ranges; r += G) {
     const int64_t p = (int64_t)r * rows + row;
     const float4 y = reinterpret_cast<const float4*>(a.part_meta)[p];
@@ -370,7 +379,7 @@ static hipError_t launch_mode(const PagedAttnArgs& a, int waves, hipStream_t str
   if (a.lq <= 16) paged_token_kernel<D, 1, DENSE, W><<<groups, 64 * W, 0, stream>>>(a);
   else paged_token_kernel<D, 2, DENSE, W><<<groups, 64 * W, 0, stream>>>(a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || a.ranges == 1) return e;
-  paged_join_kernel<D, 4><<<(int64_t)a.bh * a.lq, D / 4 * 4, 0, stream>>>(a);
+  paged_join_kernel<D, 16><<<(int64_t)a.bh * a.lq, D / 4 * 16, 0, stream>>>(a);
   return hipGetLastError();
 }
 

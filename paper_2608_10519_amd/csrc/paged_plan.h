@@ -39,7 +39,7 @@ inline size_t paged_attn_workspace(int64_t bh, int64_t lq, int64_t lk, int d, in
 // Threads of the largest launch of a call, of which there may be fewer than 2^32.
 inline int64_t paged_attn_threads(const PagedPlan& p, int64_t rows, int d) {
   if (p.waves > 1) return cache_attn_threads(p, rows, d);
-  return std::max<int64_t>(p.grid * 64 * kTokenWaves, p.ranges > 1 ? rows * d : 0);
+  return std::max<int64_t>(p.grid * 64 * kTokenWaves, p.ranges > 1 ? rows * d * 4 : 0);
 }
 
 }  // namespace sparstar

@@ -88,7 +88,7 @@ extern "C" int sparstar_rope_table(const int32_t* coords, int64_t rows, int axes
       return report_error(SPARSTAR_ERR_INVALID_ARG, "frequencies must be finite, of at most 2^20");
     const int32_t x = axis ? axis[p] : 0;
     if (x < 0 || x >= axes) return report_error(SPARSTAR_ERR_INVALID_ARG, "a pair's axis must be in [0, axes)");
-    a.turns[p] = freq[p] / 6.283185307179586477;
+    a.quarters[p] = freq[p] / 1.570796326794896619;
     a.axis[p] = uint8_t(x);
   }
   if (rows > 0 && (!coords || !table))

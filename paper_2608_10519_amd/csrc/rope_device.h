@@ -75,6 +75,11 @@ __device__ __forceinline__ uint4 turned(const ChunkTurn& u, uint4 own, uint4 oth
   return make_uint4(pack2_bf16(r[0], r[1]), pack2_bf16(r[2], r[3]), pack2_bf16(r[4], r[5]), pack2_bf16(r[6], r[7]));
 }
 
+// 16 bytes that this kernel does not read again, past the caches' share of what it does.
+__device__ __forceinline__ void store_once(uint16_t* p, uint4 r) {
+  __builtin_nontemporal_store((u32x4){r.x, r.y, r.z, r.w}, reinterpret_cast<u32x4*>(p));
+}
+
 // Work-groups are launched in rows of at most 2^20: a launch may have fewer than 2^32 threads
 // along each axis.
 inline dim3 rows_of_groups(int64_t n) {
@@ -83,5 +88,34 @@ inline dim3 rows_of_groups(int64_t n) {
   return dim3((uint32_t)((n + rows - 1) / rows), (uint32_t)rows);
 }
 __device__ __forceinline__ int64_t group_of_rows() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+// a / b of numbers that mostly fit 32 bits, where a division takes a fifth of the instructions.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// The work of a thread of a launch over (group of heads, token of any batch element, chunk):
+// work-groups take 256 / cpr tokens of one group.
+struct TokenChunk {
+  int64_t group, at, b, l;  // at = b L + l
+  int c;
+  bool ok;
+};
+__device__ __forceinline__ TokenChunk token_chunk(int64_t tokens, int64_t len, int cpr_bits) {
+  const int tpg = 256 >> cpr_bits;
+  const int64_t per_group = (tokens + tpg - 1) / tpg, w = group_of_rows();
+  TokenChunk t;
+  t.group = divide(w, per_group);
+  t.at = (w - t.group * per_group) * tpg + (threadIdx.x >> cpr_bits);
+  t.c = threadIdx.x & ((1 << cpr_bits) - 1);
+  t.ok = t.at < tokens;
+  t.b = tokens == len ? 0 : divide(t.at, len);
+  t.l = t.at - t.b * len;
+  return t;
+}
+inline dim3 token_grid(int64_t groups, int64_t tokens, int d) {
+  const int tpg = 256 / (d / 8);
+  return rows_of_groups(groups * ((tokens + tpg - 1) / tpg));
+}
 
 }  // namespace sparstar
