@@ -67,12 +67,13 @@ struct PagedAttnArgs : CacheAttnArgs {
   const int32_t* pages;            // [B, n_table]
   int64_t n_table, n_pages;
   float* part32;                   // up to 32 rows: fp32 partial results [ranges, BH, Lq, D]
+  int waves, token_waves;          // of a work-group (launcher only), as in PagedPlan
 };
 
 hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 hipError_t launch_paged_write(const PagedArgs& a, hipStream_t stream);
 hipError_t launch_paged_read(const PagedArgs& a, hipStream_t stream);
-hipError_t launch_paged_attn(const PagedAttnArgs& a, int d, int waves, bool dense, hipStream_t stream);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, int d, bool dense, hipStream_t stream);
 
 }  // namespace sparstar

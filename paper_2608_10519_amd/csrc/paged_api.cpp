@@ -171,12 +171,14 @@ static int paged_attn_common(const void* q, const void* k_pages, const void* v_p
   a.rotation = plan.rotation;
   a.spread_bits = plan.spread_bits;
   a.grid = plan.grid;
+  a.waves = plan.waves;
+  a.token_waves = plan.token_waves;
   if (plan.ranges > 1) {
     a.part_o = static_cast<uint16_t*>(workspace);  // (more than 32 rows)
     a.part32 = static_cast<float*>(workspace);
     a.part_meta = reinterpret_cast<float*>(static_cast<char*>(workspace) + paged_part_bytes(bh * Lq, Lq, D, plan.ranges));
   }
-  const hipError_t e = launch_paged_attn(a, D, plan.waves, dense, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_paged_attn(a, D, dense, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return report_error(SPARSTAR_ERR_HIP, hipGetErrorString(e));
   return clear_error();
 }

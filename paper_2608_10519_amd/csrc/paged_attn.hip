@@ -23,8 +23,10 @@ __device__ __forceinline__ uint32_t scale_byte(__amdgpu_buffer_rsrc_t rs, int at
 //     them and stores them as bf16 rows, which the transpose read takes by columns.  A product
 //     with ones sums the rounded P.
 template <int D, int NC, bool DENSE, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(D * NC > 128 ? 1 : 2, 2)))
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_token_kernel(PagedAttnArgs a) {
+  // tiles whose loads are in flight: 32 rows at D = 128 have no registers for two
+  constexpr int AHEAD = D * NC > 128 ? 1 : 2;
   constexpr int KS = D / 32;           // k-steps of S
   constexpr int DT = D / 16;           // 16-channel tiles of O^T
   constexpr int KW = D / 32;           // dwords of K codes per lane and 16 keys
@@ -164,16 +166,17 @@ void paged_token_kernel(PagedAttnArgs a) {
   auto step = [&](Tile cur, const Raw& r) {
     f32x4 s[4][NC];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float sc = __uint_as_float(r.ks[u] << 23);
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int c = 0; c < NC; ++c) s[u][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const bf16x8 kv = decode8_4bit(r.k[u][k], sc);
+    for (int n = 0; n < 4 * KS; ++n) {
+      // the four sums in turn, so that a product waits for none of its neighbours (two columns
+      // are two sums already, and have no registers for more)
+      const int u = NC == 1 ? n % 4 : n / KS, k = NC == 1 ? n / 4 : n % KS;
+      const bf16x8 kv = decode8_4bit(r.k[u][k], __uint_as_float(r.ks[u] << 23));
 #pragma unroll
-        for (int c = 0; c < NC; ++c) s[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qf[c][k], s[u][c], 0, 0, 0);
-      }
+      for (int c = 0; c < NC; ++c) s[u][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qf[c][k], s[u][c], 0, 0, 0);
     }
 #pragma unroll
     for (int u = 0; u < VL; ++u) {
@@ -249,26 +252,32 @@ void paged_token_kernel(PagedAttnArgs a) {
 
   if (first < end) {
     load_batch(first >> sub_bits);
+    // (A tile's loads stay in the order of the tiles, which is that of the waits.)
+    auto next = [&](int i, Tile& t, Raw& r) {
+      __builtin_amdgcn_sched_barrier(0);
+      t = fetch(i);
+      load(t, r);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    Tile t0, t1;
     Raw r0, r1;
-    Tile t0 = fetch(first), t1 = fetch(first + 1);
-    load(t0, r0);
-    __builtin_amdgcn_sched_barrier(0);  // (a tile's loads stay in the order of the tiles, which is that of the waits)
-    load(t1, r1);
-    __builtin_amdgcn_sched_barrier(0);
-    int i = first;
-    for (; i + 1 < end; i += 2) {  // (no way out in between, which would make every wait one for all loads)
-      step(t0, r0);
-      __builtin_amdgcn_sched_barrier(0);
-      t0 = fetch(i + 2);
-      load(t0, r0);
-      __builtin_amdgcn_sched_barrier(0);
-      step(t1, r1);
-      __builtin_amdgcn_sched_barrier(0);
-      t1 = fetch(i + 3);
-      load(t1, r1);
-      __builtin_amdgcn_sched_barrier(0);
+    next(first, t0, r0);
+    if constexpr (AHEAD == 1) {
+      for (int i = first; i < end; ++i) {
+        step(t0, r0);
+        next(i + 1, t0, r0);
+      }
+    } else {
+      next(first + 1, t1, r1);
+      int i = first;
+      for (; i + 1 < end; i += 2) {  // (no way out in between, which would make every wait one for all loads)
+        step(t0, r0);
+        next(i + 2, t0, r0);
+        step(t1, r1);
+        next(i + 3, t1, r1);
+      }
+      if (i < end) step(t0, r0);
     }
-    if (i < end) step(t0, r0);
   }
 
   // The waves join: with M = max_w m_w, sums of 2^(m_w - M) times each one's, every wave for some
@@ -325,7 +334,9 @@ void paged_token_kernel(PagedAttnArgs a) {
   }
 }
 
-// Joins the ranges of a row, D / 4 threads and G groups of them, each over every G-th range.
+// Joins the ranges of a row, D / 4 threads and G groups of them, each over every G-th range: with
+// 16 a thread reads four at most, all at once (64 ranges of one row 8.7 us with four groups).
+constexpr int kJoinGroups = 16;
 template <int D, int G>
 __global__ __launch_bounds__(D / 4 * G) void paged_join_kernel(PagedAttnArgs a) {
   constexpr int LPR = D / 4;
@@ -371,21 +382,26 @@ __global__ __launch_bounds__(D / 4 * G) void paged_join_kernel(PagedAttnArgs a) 
   if (a.lse != nullptr && c == 0) a.lse[row] = le == 0.f ? -INFINITY : (mm + log2f(le)) * 0.69314718055994530942f;
 }
 
-template <int D, bool DENSE>
-static hipError_t launch_mode(const PagedAttnArgs& a, int waves, hipStream_t stream) {
-  if (waves > 1) return launch_rows<D, DENSE, Codes4>(a, waves, stream);
+template <int D, bool DENSE, int W>
+static hipError_t launch_token(const PagedAttnArgs& a, hipStream_t stream) {
   const int64_t groups = (int64_t)a.bh * a.ranges;
-  constexpr int W = kTokenWaves;
   if (a.lq <= 16) paged_token_kernel<D, 1, DENSE, W><<<groups, 64 * W, 0, stream>>>(a);
   else paged_token_kernel<D, 2, DENSE, W><<<groups, 64 * W, 0, stream>>>(a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || a.ranges == 1) return e;
-  paged_join_kernel<D, 16><<<(int64_t)a.bh * a.lq, D / 4 * 16, 0, stream>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_paged_attn(const PagedAttnArgs& a, int d, int waves, bool dense, hipStream_t stream) {
-  if (d == 128) return dense ? launch_mode<128, true>(a, waves, stream) : launch_mode<128, false>(a, waves, stream);
-  return dense ? launch_mode<64, true>(a, waves, stream) : launch_mode<64, false>(a, waves, stream);
+template <int D, bool DENSE>
+static hipError_t launch_mode(const PagedAttnArgs& a, hipStream_t stream) {
+  if (a.waves > 1) return launch_rows<D, DENSE, Codes4>(a, a.waves, stream);
+  const hipError_t e = a.token_waves == 8 ? launch_token<D, DENSE, 8>(a, stream) : launch_token<D, DENSE, 4>(a, stream);
+  if (e != hipSuccess || a.ranges == 1) return e;
+  paged_join_kernel<D, kJoinGroups><<<(int64_t)a.bh * a.lq, D / 4 * kJoinGroups, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_attn(const PagedAttnArgs& a, int d, bool dense, hipStream_t stream) {
+  if (d == 128) return dense ? launch_mode<128, true>(a, stream) : launch_mode<128, false>(a, stream);
+  return dense ? launch_mode<64, true>(a, stream) : launch_mode<64, false>(a, stream);
 }
 
 }  // namespace sparstar

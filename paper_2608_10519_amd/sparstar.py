@@ -11,6 +11,7 @@ gradient call of the same name joins them (README.md has one).
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -109,7 +110,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.sparstar_cache_dense_attn_fwd.restype = c_i
     lib.sparstar_rope_frequencies.argtypes = [c_i] + [ctypes.c_double] * 5 + [c_dp]
     lib.sparstar_rope_frequencies.restype = c_i
-    lib.sparstar_rope_table.argtypes = [c_p, c_i64, c_i, c_i, c_dp, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, c_p, c_p]
+    lib.sparstar_rope_table.argtypes = [c_p, c_i64, c_i, c_i, c_p, c_p, ctypes.c_double, c_p, c_p]
     lib.sparstar_rope_table.restype = c_i
     for fn in (lib.sparstar_rope_fwd, lib.sparstar_rope_bwd):
         fn.argtypes = [c_p, Strides, c_i, c_i, c_i64, c_i, c_p, c_i64, c_i, c_i, c_p, c_i64, c_p, Strides, c_p]
@@ -392,7 +393,7 @@ def _like(t: torch.Tensor | None, shape, dtype, name: str, device: torch.device)
 
 def _launch(fn: str, device: torch.device, *args) -> None:
     """Calls the library on the device's current stream (and with the device current)."""
-    if device.index == torch.cuda.current_device():
+    if device.index == torch._C._cuda_getDevice():
         rc = getattr(load(), fn)(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
         with torch.cuda.device(device):
@@ -594,26 +595,28 @@ def sparstar_rope_table(coords: torch.Tensor, freq: Sequence[float], axis: Seque
     (rows, axes), pairs, dev = coords.shape, len(freq), coords.device
     table = torch.empty((rows, pairs, 2), dtype=torch.float32, device=dev) if out is None else out
     tp = _like(table, (rows, pairs, 2), torch.float32, "out", dev)
-    f = (ctypes.c_double * max(pairs, 1))(*freq)
-    ax = (ctypes.c_int32 * max(pairs, 1))(*axis) if axis is not None else None
-    _launch("sparstar_rope_table", dev, coords.data_ptr(), rows, axes, pairs, f, ax, float(amplitude), tp)
+    f, ax = array.array("d", freq), array.array("i", axis) if axis is not None else None  # (held to the end of the call)
+    _launch("sparstar_rope_table", dev, coords.data_ptr(), rows, axes, pairs, f.buffer_info()[0],
+            ax.buffer_info()[0] if ax is not None else None, float(amplitude), tp)
     return table
 
 
 def _strided(t: torch.Tensor, name: str, device: torch.device | None = None, shape=None) -> Strides:
     """Strides of a bf16 tensor [B, H, L, D] on the GPU whose rows are contiguous."""
-    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+    s = t.stride()
+    if t.dtype is not torch.bfloat16 or not t.is_cuda or len(s) != 4 or s[3] != 1:
         raise ValueError(f"{name} must be a 4-D bf16 tensor on the GPU [B, H, L, D] with contiguous rows")
     if device is not None and (t.device != device or t.shape != shape):
         raise ValueError(f"{name} must be a tensor on {device} of shape {tuple(shape)}")
-    return Strides(*t.stride()[:3])
+    return Strides(s[0], s[1], s[2])
 
 
 def _table(table: torch.Tensor, device: torch.device) -> tuple[int, int, int]:
     """(pointer, rows, pairs) of a table."""
     if table.dim() != 3:
         raise ValueError("the table must be [rows, pairs, 2]")
-    return _like(table, (*table.shape[:2], 2), torch.float32, "table", device), table.shape[0], table.shape[1]
+    rows, pairs, _ = table.shape
+    return _like(table, (rows, pairs, 2), torch.float32, "table", device), rows, pairs
 
 
 def _rope(fn, x, table, start, positions, interleaved, out):
@@ -621,8 +624,10 @@ def _rope(fn, x, table, start, positions, interleaved, out):
     B, H, L, D = x.shape
     tp, rows, pairs = _table(table, dev)
     pp = _like(positions, (B, L), torch.int32, "positions", dev)
-    y = torch.empty((B, H, L, D), dtype=torch.bfloat16, device=dev) if out is None else out
-    ys = _strided(y, "out", dev, x.shape)
+    if out is None:
+        y, ys = torch.empty_like(x, memory_format=torch.contiguous_format), Strides(H * L * D, L * D, D)
+    else:
+        y, ys = out, _strided(out, "out", dev, x.shape)
     _launch(fn, dev, x.data_ptr(), xs, B, H, L, D, tp, rows, pairs, int(interleaved), pp, start, y.data_ptr(), ys)
     return y
 
@@ -670,14 +675,14 @@ class PagedCache(NamedTuple):
 
 def _paged(c: PagedCache, pages: torch.Tensor, B: int, H: int, D: int, device: torch.device):
     """(pages, n_table, n_pages) and the four pointers of a cache that fits B, H and D."""
-    if c.k.dim() != 4 or pages.dim() != 2:
+    k, v, k_scale, v_scale = c
+    if k.dim() != 4 or pages.dim() != 2:
         raise ValueError("the cache's k must be [n_pages, H, block_size, D / 2], pages [B, n_table]")
-    n, u8, b = c.k.shape[0], torch.uint8, c.k.shape[2]
-    codes, scale = (n, H, b, D // 2), (n, H, b, D // 32)
-    ptrs = (_like(c.k, codes, u8, "cache.k", device), _like(c.v, codes, u8, "cache.v", device),
-            _like(c.k_scale, scale, u8, "cache.k_scale", device), _like(c.v_scale, scale, u8, "cache.v_scale", device))
-    table = _like(pages, (B, pages.shape[1]), torch.int32, "pages", device)
-    return (table, pages.shape[1], n), ptrs
+    n, _, b, _ = k.shape
+    n_table, u8, codes, scale = pages.shape[1], torch.uint8, (n, H, b, D // 2), (n, H, b, D // 32)
+    ptrs = (_like(k, codes, u8, "cache.k", device), _like(v, codes, u8, "cache.v", device),
+            _like(k_scale, scale, u8, "cache.k_scale", device), _like(v_scale, scale, u8, "cache.v_scale", device))
+    return (_like(pages, (B, n_table), torch.int32, "pages", device), n_table, n), ptrs
 
 
 def sparstar_paged_write(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, pages: torch.Tensor, start: int = 0, *,
