@@ -242,6 +242,13 @@ void cache_attn_kernel(typename F::Args a) {
   constexpr int SUB = (DENSE ? 64 : ROWS) / C::KB;  // tiles per entry (dense: of 64 keys)
   const int64_t scale_at = bh * ((a.cap + a.block - 1) / a.block);
   int breg = -1, sreg = 0, lbase = 0;
+  const int32_t* page_row = nullptr;
+  uint32_t head_of = 0;
+  if constexpr (F::PAGED) {
+    const uint32_t seq = (uint32_t)bh / (uint32_t)a.heads;
+    head_of = (uint32_t)bh - seq * (uint32_t)a.heads;
+    page_row = a.pages + seq * a.n_table;
+  }
   // (dense entries are 64 keys whatever the block size)
   const int e_bits = DENSE ? (a.block == 128 ? 1 : 0) : 0;
   if constexpr (DENSE) {
@@ -258,7 +265,7 @@ void cache_attn_kernel(typename F::Args a) {
     const int blk = b >> e_bits;
     if (b < 0 || blk >= n_blk) b = -1;
     if constexpr (F::PAGED) {
-      sreg = b < 0 ? -1 : a.pages[bh / a.heads * a.n_table + blk];
+      sreg = b < 0 ? -1 : page_row[blk];
       if (sreg < 0 || sreg >= a.n_pages) b = -1, sreg = 0;
     } else {
       sreg = 127 | 127 << 8;
@@ -289,7 +296,7 @@ void cache_attn_kernel(typename F::Args a) {
     const uint32_t n = (uint32_t)t.t < n_whole ? C::KB * D : ((uint32_t)t.t == n_whole ? last_codes : 0u);
     if constexpr (F::PAGED) {
       // (tiles per page: a power of two)
-      const int64_t row = ((int64_t)t.s * a.heads + bh % a.heads) * a.block + (t.t & (a.block / C::KB - 1)) * C::KB;
+      const int64_t row = ((int64_t)t.s * a.heads + head_of) * a.block + (t.t & (a.block / C::KB - 1)) * C::KB;
       const auto rs = tile_rsrc(codes + row * (D / 2), n / 2), rss = tile_rsrc(scales + row * (D / 32), n / 32);
 #pragma unroll
       for (int i = 0; i < C::CV; ++i) {

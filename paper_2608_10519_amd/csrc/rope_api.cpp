@@ -28,7 +28,7 @@ int check_strides(sparstar_strides s, int B, int H, int64_t L, int D, bool outpu
     if (x.size > 1 && x.stride > ((int64_t(1) << 46) - reach) / (x.size - 1)) return refuse("tensor too large");
     if (x.size > 1) reach += x.stride * (x.size - 1);
   }
-  if (!output) return SPARSTAR_OK;
+  if (!output || L == 0) return SPARSTAR_OK;  // (no rows that could overlap)
   std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
   int64_t within = D;  // elements from the first to the last of the dimensions so far
   for (const Dim& x : d) {

@@ -714,7 +714,9 @@ def sparstar_paged_read(cache: PagedCache, pages: torch.Tensor, start: int, L: i
     shape = (B, H, L, D)
     if out is None:
         out = [torch.empty(shape, dtype=bf16, device=dev) if n in want else None for n in ("k", "v")]
-    kp, vp = _like(out[0], shape, bf16, "k", dev), _like(out[1], shape, bf16, "v", dev)
+        kp, vp = (t.data_ptr() if t is not None else None for t in out)
+    else:
+        kp, vp = _like(out[0], shape, bf16, "k", dev), _like(out[1], shape, bf16, "v", dev)
     _launch("sparstar_paged_read", dev, *ptrs, B, H, start, L, D, cache.block_size, *where, kp, vp)
     return tuple(out)
 
@@ -741,16 +743,22 @@ def _paged_attn(fn, q, cache, pages, lists, Lk, softmax_scale, lens, out, lse, r
     lp = _like(lens, (B,), torch.int32, "lens", dev)
     listed = _lists(*lists, B, H, Lq, b, dev) if lists is not None else ()
     o = torch.empty_like(q) if out is None else out
-    if lse is None and return_lse:
+    op = o.data_ptr() if out is None else _like(out, q.shape, torch.bfloat16, "out", dev)
+    if lse is not None:
+        lsep = _like(lse, (B, H, Lq), torch.float32, "lse", dev)
+    elif return_lse:
         lse = torch.empty((B, H, Lq), dtype=torch.float32, device=dev)
-    op, lsep = _like(o, q.shape, torch.bfloat16, "out", dev), _like(lse, (B, H, Lq), torch.float32, "lse", dev)
+        lsep = lse.data_ptr()
+    else:
+        lsep = None
     wp, wn = None, 0
     if split:
-        if workspace is None:
-            need = _paged_scratch(B, H, Lq, Lk, D, b, listed[2] if listed else 0)
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
         if workspace is not None:
             wp, wn = _scratch(workspace, dev)
+        else:
+            wn = _paged_scratch(B, H, Lq, Lk, D, b, listed[2] if listed else 0)
+            workspace = torch.empty(wn, dtype=torch.uint8, device=dev) if wn else None
+            wp = workspace.data_ptr() if wn else None
     _launch(fn, dev, q.data_ptr(), *ptrs, B, H, Lq, Lk, D, b, *where, lp, *listed, float(softmax_scale), op, lsep, wp, wn)
     return o, lse
 

@@ -106,6 +106,7 @@ def test_rotations_refuse(lib, back, over, msg):
 
 def test_rotation_of_nothing(lib):
     assert _rope(lib, L=0, x=None, y=None, start=20) == S.OK
+    assert _rope(lib, L=0, x=None, y=None, ys=S.Strides(0, 0, 64)) == S.OK  # as a dense tensor without tokens has them
     # strides of sizes of one do not matter
     assert _rope(lib, B=1, H=1, L=0, xs=S.Strides(-3, 7, 5), ys=S.Strides(1, 2, 3), x=None, y=None) == S.OK
 
