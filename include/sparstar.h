@@ -600,9 +600,9 @@ size_t sparstar_paged_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk,
  * j of sequence b is the page pages[b, j].  Arguments, roundings and results are those of the
  * 8-bit cache's calls, but for
  *   pages, n_table  device int32 [B, n_table], Lk <= n_table * block_size
- *   workspace       of sparstar_paged_attn_workspace_bytes(...); up to 32 query rows the
- *                   ranges' sums are kept in fp32 there, for more in fp16 as there
- * and P, which is not rounded where a single row attends (Lq = 1).
+ *   kv_stride       at most 2^28
+ *   workspace       of sparstar_paged_attn_workspace_bytes(...) bytes; up to 32 query rows
+ *                   the ranges' sums are kept in fp32 there, of more rows in fp16 as there.
  */
 int sparstar_paged_sparse_attn_fwd(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
                                    const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int D,

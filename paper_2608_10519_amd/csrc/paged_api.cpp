@@ -130,7 +130,8 @@ static int paged_attn_common(const void* q, const void* k_pages, const void* v_p
   if (!dense && Lq > 0) {
     if (!kv_num_blocks || !kv_indices)
       return report_error(SPARSTAR_ERR_INVALID_ARG, "kv_num_blocks and kv_indices must be non-null");
-    if (kv_stride < 1) return report_error(SPARSTAR_ERR_INVALID_ARG, "kv_stride must be >= 1");
+    if (kv_stride < 1 || kv_stride > (1 << 28))
+      return report_error(SPARSTAR_ERR_INVALID_ARG, "kv_stride must be in [1, 2^28]");
   }
   if (!(softmax_scale == softmax_scale) || isinf(softmax_scale))
     return report_error(SPARSTAR_ERR_INVALID_ARG, "softmax_scale must be finite");

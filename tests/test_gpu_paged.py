@@ -324,6 +324,62 @@ def test_offsets_past_32_bits(gpu_lib, Lq):
     assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
+JOINS = [  # D, block, H, Lq, Lk, list length (0: dense), ranges
+    (128, 64, 1, 1, 9000, 0, 8), (64, 128, 2, 7, 9000, 30, 3), (128, 128, 3, 32, 14_000, 0, 13), (64, 64, 2, 17, 9000, 60, 3),
+    (128, 128, 1, 100, 9000, 0, None), (64, 64, 1, 64, 9000, 60, None), (128, 64, 18, 220, 3500, 0, None),
+    (64, 64, 3, 300, 9000, 0, None),
+]
+
+
+@pytest.mark.parametrize("D,block,H,Lq,Lk,stride,ranges", JOINS)
+def test_ranges_join(gpu_lib, D, block, H, Lq, Lk, stride, ranges):
+    got = gpu_lib.load().sparstar_internal_paged_ranges(1, H, Lq, Lk, D, block, stride)
+    _say(f"[paged ranges] {(D, block, H, Lq, Lk, stride)}: {got}")
+    assert got > 1 and ranges in (None, got)
+    g = torch.Generator().manual_seed(Lk + Lq)
+    n = -(-Lk // block)
+    c = pool(gpu_lib, g, n, H, D, block)
+    pages = own_pages(g, 1, n, n)
+    q = torch.randn(1, H, Lq, D, generator=g).bfloat16()
+    lists = None
+    if stride:
+        lists = [[[sorted(torch.randperm(n, generator=g)[:stride].tolist()) for _ in range(-(-Lq // block))] for _ in range(H)]]
+    o, lse = attend(gpu_lib, q.cuda(), c, pages.cuda(), lists, Lk, 1 / math.sqrt(D), None)
+    check(o, lse, q, c, pages, lists, [Lk], 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("Lq", [5, 20, 60])
+def test_a_nan_query_stays_in_its_row(gpu_lib, Lq):
+    D, block, H, Lk = 128, 64, 2, 900
+    g = torch.Generator().manual_seed(9)
+    c = pool(gpu_lib, g, 15, H, D, block)
+    pages = own_pages(g, 1, 15, 15)
+    q = torch.randn(1, H, Lq, D, generator=g).bfloat16()
+    clean = q.clone()
+    q[0, 0, 3, 17] = math.nan
+    o, lse = attend(gpu_lib, q.cuda(), c, pages.cuda(), None, Lk, 1 / math.sqrt(D), None)
+    assert o[0, 0, 3].isnan().all() and lse[0, 0, 3].isnan()
+    o[0, 0, 3], lse[0, 0, 3] = 0.0, 0.0
+    assert not o.isnan().any() and not lse.isnan().any()
+    good = torch.arange(Lq) != 3
+    check(o[:, :, good], lse[:, :, good], clean[:, :, good], c, pages, None, [Lk], 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("Lq", [1, 20])
+def test_many_heads(gpu_lib, Lq):
+    """More heads than work-groups at once, of short sequences of every length."""
+    D, block, B, H, n = 64, 64, 40, 24, 3
+    g = torch.Generator().manual_seed(10)
+    c = pool(gpu_lib, g, B * n, H, D, block)
+    pages = own_pages(g, B, n, B * n)
+    lens = [(7 * b) % (n * block + 1) for b in range(B)]
+    q = torch.randn(B, H, Lq, D, generator=g).bfloat16()
+    o, lse = attend(gpu_lib, q.cuda(), c, pages.cuda(), None, n * block, 1 / math.sqrt(D),
+                    torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    pick = [0, 1, 9, 28, 39]
+    check(o[pick], lse[pick], q[pick], c, pages[pick], None, [lens[b] for b in pick], 1 / math.sqrt(D))
+
+
 @pytest.mark.parametrize("Lq", [1, 5, 130])
 def test_a_step_as_it_is_used(gpu_lib, Lq):
     """Rotation out of a fused projection, append, read for the selector, block-sparse attention:

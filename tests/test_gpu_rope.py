@@ -190,3 +190,19 @@ def test_streams_devices_and_graphs(gpu_lib):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, eager) and torch.equal(dx, want_dx) and (dqkv[:, :, 1:] == 0).all()
+
+
+def test_more_work_groups_than_a_row_of_them(gpu_lib):
+    """2^25 tokens: work-groups past 2^20, offsets past 2^32 bytes, in place."""
+    L, D = (1 << 25) + 700, 64
+    g = torch.Generator().manual_seed(12)
+    table = P.random_table(g, 97, 32)
+    pos = (torch.arange(L, dtype=torch.int32, device="cuda") % 97)[None].contiguous()
+    x = torch.empty(1, 1, L, D, dtype=torch.bfloat16, device="cuda")
+    rows = torch.randn(1, 1, 300, D, generator=g).bfloat16()
+    at = [0, (1 << 25) - 150, L - 300]
+    for i in at:
+        x[:, :, i: i + 300] = rows.cuda()
+    gpu_lib.sparstar_rope_fwd(x, table.cuda(), positions=pos, out=x)
+    for i in at:
+        assert torch.equal(x[:, :, i: i + 300].cpu(), P.turn(rows, table[torch.arange(i, i + 300) % 97], 32))

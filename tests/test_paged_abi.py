@@ -194,10 +194,36 @@ def test_paged_attention_refuses(lib, is_dense, over, code, msg):
 
 
 @pytest.mark.parametrize("over,msg", [(dict(num=None), "kv_num_blocks"), (dict(idx=None), "kv_indices"),
-                                      (dict(stride=0), "kv_stride")])
+                                      (dict(stride=0), "kv_stride"), (dict(stride=(1 << 28) + 1), "kv_stride")])
 def test_sparse_paged_attention_refuses_lists(lib, over, msg):
     assert _attend(lib, **over) == S.ERR_INVALID_ARG
     assert msg in S.last_error()
+
+
+def test_workspaces(lib):
+    """A workspace is asked for where a call may be cut, and has to be that large."""
+    size = S.sparstar_paged_attn_workspace_bytes
+    assert size(1, 2, 5, 128, 96, 64) == size(0, 2, 5, 128, 64, 64) == size(1, 2, 5, 0, 64, 64) == 0
+    assert size(1, 1, 1, 64, 64, 64) == 0
+    for Lq in (1, 32, 33, 300):
+        n = size(1, 2, Lq, 9000, 64, 64)
+        assert n > 0 and size(2, 2, Lq, 9000, 64, 64) >= n
+        for is_dense in (False, True):
+            over = dict(Lq=Lq, Lk=9000, n_table=200, ws=FAKE, ws_bytes=n - 1)
+            assert _attend(lib, is_dense, **over) == S.ERR_WORKSPACE
+            assert "smaller" in S.last_error()
+
+
+def test_ranges_fill_the_chip(lib):
+    """Cuts by the rule: none for short lists, whole work-groups over the 256 CUs for long ones."""
+    cut = lib.sparstar_internal_paged_ranges
+    assert cut(1, 8, 1, 1152, 64, 64, 0) == 1
+    assert cut(2, 24, 1, 84_032, 128, 64, 0) == 10  # 480 work-groups of four waves, two to a CU
+    assert cut(1, 1, 7, 144_512, 128, 64, 0) == 64
+    assert cut(1, 24, 1, 144_512, 128, 64, 20) == 1  # short lists of a long cache
+    assert cut(600, 1, 1, 144_512, 128, 64, 0) == 1
+    assert cut(1, 24, 128, 144_512, 128, 64, 0) == 21  # 504 work-groups of 128 rows
+    assert cut(1, 18, 220, 10_061, 128, 64, 0) == 14
 
 
 # ---- the binding's own checks
