@@ -314,27 +314,33 @@ void cache_attn_kernel(typename F::Args a) {
   auto load_v = [&](Tile t, Piece (&u)[C::CV]) { load_raw(a.v_cache, a.v_scale, t, u); };
 
   // ---- converted tiles: rows of 2 D bytes whose 16-byte chunks are permuted as in
-  // attn_fwd.hip, chunk c of K row r at c ^ kswz(r), of V row r at c ^ vswz(r)
+  // attn_fwd.hip, chunk c of K row r at c ^ kswz(r), of V row r at c ^ vswz(r).  A store of 16
+  // bytes a lane takes eight lanes at a time, over 128 bytes of banks: a lane's first piece is
+  // an even chunk, so those of the second half of 256 bytes are moved to the odd ones (without
+  // it every store took twice its eight cycles, an eighth of the dense kernel's cycles).
   constexpr int CRB = 2 * D, CRPB = 256 / CRB, CCPR = D / 8;
   auto kswz = [](int r) { return (r / CRPB) % CCPR; };
   auto vswz = [](int r) { return (((r / CRPB) & 3) << 2) & (CCPR - 1); };
+  auto half = [](int r, int c) { return D == 128 ? c >> 3 : r & 1; };
   uint32_t koff[C::DS];  // K row l32, chunk 2 s + h
 #pragma unroll
-  for (int s = 0; s < C::DS; ++s) koff[s] = (uint32_t)(l32 * CRB + 16 * ((2 * s + hh) ^ kswz(l32)));
+  for (int s = 0; s < C::DS; ++s) koff[s] = (uint32_t)(l32 * CRB + 16 * ((2 * s + hh) ^ kswz(l32) ^ half(l32, 2 * s + hh)));
   uint32_t voff[C::DT];  // transpose read: rows 4 h + (0..3), columns 32 t + l % 32
   {
     const int sl = lane & 15, r = 4 * hh + (sl >> 2);
 #pragma unroll
-    for (int t = 0; t < C::DT; ++t)
-      voff[t] = (uint32_t)(r * CRB + 16 * ((4 * t + 2 * (lane >> 4 & 1) + ((sl & 3) >> 1)) ^ vswz(r)) + 8 * (sl & 1));
+    for (int t = 0; t < C::DT; ++t) {
+      const int c = 4 * t + 2 * (lane >> 4 & 1) + ((sl & 3) >> 1);
+      voff[t] = (uint32_t)(r * CRB + 16 * (c ^ vswz(r) ^ half(r, c)) + 8 * (sl & 1));
+    }
   }
   // Where the lane's pieces go: to two neighbouring chunks, 8 (D = 64: 16) rows further per
   // i, which moves kswz by 8 chunks of 16 (D = 128) or not at all, and leaves vswz as it is.
   uint32_t kdst, vdst;
   {
     const int r = src / D, c = 2 * (src % D / 16);
-    kdst = (uint32_t)(r * CRB + 16 * (c ^ kswz(r)));
-    vdst = (uint32_t)(r * CRB + 16 * (c ^ vswz(r)));
+    kdst = (uint32_t)(r * CRB + 16 * (c ^ kswz(r) ^ half(r, c)));
+    vdst = (uint32_t)(r * CRB + 16 * (c ^ vswz(r) ^ half(r, c)));
   }
   auto convert = [&](const Piece& p, int byte, char* tile, uint32_t dst) {
     if constexpr (F::PAGED) {

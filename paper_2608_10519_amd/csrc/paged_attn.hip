@@ -136,17 +136,18 @@ void paged_token_kernel(PagedAttnArgs a) {
   };
 
   // V in LDS: the chunks of row r are permuted so that eight consecutive rows' pairs of chunks
-  // (the transpose read) and two rows' chunks four apart (the stores) fall on different banks.
-  auto swz = [](int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
+  // (the transpose read, 256 bytes of banks) and what eight lanes store (chunks four apart of two
+  // rows, or of four at D = 64, 128 bytes of banks) fall on different ones.
+  auto swz = [](int r, int c) { return D == 128 ? 2 * (r & 7) ^ c >> 3 : 2 * ((r >> 1) & 3) ^ (r & 1); };
   uint8_t* const vt = tiles[wave];
   const int vrow = lane / LPK, vc = 4 * (lane % LPK);
   uint32_t vput[4], vget[DT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) vput[i] = (uint32_t)(vrow * RB + 16 * ((vc + i) ^ swz(vrow)));
+  for (int i = 0; i < 4; ++i) vput[i] = (uint32_t)(vrow * RB + 16 * ((vc + i) ^ swz(vrow, vc + i)));
   {
     const int r = 4 * j + (lane & 15) / 4, p = lane & 3;  // rows 4 j .. + 3, four pieces of 8 bytes
 #pragma unroll
-    for (int t = 0; t < DT; ++t) vget[t] = (uint32_t)(r * RB + 16 * ((2 * t + p / 2) ^ swz(r)) + 8 * (p % 2));
+    for (int t = 0; t < DT; ++t) vget[t] = (uint32_t)(r * RB + 16 * ((2 * t + p / 2) ^ swz(r, 2 * t + p / 2)) + 8 * (p % 2));
   }
   auto read_v = [&](int t, int half) -> bf16x8 {
     const uint16_t* p = reinterpret_cast<const uint16_t*>(vt + vget[t] + 32 * half * RB);
