@@ -204,10 +204,11 @@ void cache_attn_kernel(typename F::Args a) {
   // tokens that exist: rows past them are neither read nor attended to
   int64_t len = a.lk;
   if (a.lens != nullptr) {
-    const int n = a.lens[bh / a.heads];
+    const int n = a.lens[(uint32_t)bh / (uint32_t)a.heads];
     len = n < 0 ? 0 : (n < a.lk ? n : a.lk);
   }
-  const int n_blk = (int)((len + a.block - 1) / a.block);
+  const int block_bits = a.block == 128 ? 7 : 6;
+  const int n_blk = (int)((len + a.block - 1) >> block_bits);
 
   // ---- Q as the B operand of S^T = K Q^T: Q[q][16 s + 8 h .. +7]
   const int64_t row = (int64_t)qg * ROWS + wave * 32 + l32;
@@ -232,21 +233,27 @@ void cache_attn_kernel(typename F::Args a) {
       n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
       list = a.kv_indices + r * a.stride;
     }
-    first = __builtin_amdgcn_readfirstlane((int)((int64_t)n * range / a.ranges));
-    cnt = __builtin_amdgcn_readfirstlane((int)((int64_t)n * (range + 1) / a.ranges)) - first;
+    // (a 64-bit division is some 150 scalar instructions)
+    auto part = [&](int r) -> int {
+      if (n < 1 << 25) return (int)((uint32_t)n * (uint32_t)r / (uint32_t)a.ranges);
+      return (int)((int64_t)n * r / a.ranges);
+    };
+    first = __builtin_amdgcn_readfirstlane(part(range));
+    cnt = __builtin_amdgcn_readfirstlane(part(range + 1)) - first;
     if (!DENSE && a.rotation > 0 && n < n_blk)
       rot = (int)((int64_t)(gi % (uint32_t)a.rotation) * cnt / a.rotation);
   }
-  // Entries 64 at a time in VGPRs: the block and its scale bytes, or its page.  One that names
-  // no block (page) gives -1, whose tiles are loaded as zeros and masked.
+  // Entries 64 at a time in VGPRs: the block and its scale bytes, or its page's first tile in the
+  // pool (which holds less than 2^31).  One that names no block (page) gives -1, whose tiles are
+  // loaded as zeros and masked.
   constexpr int SUB = (DENSE ? 64 : ROWS) / C::KB;  // tiles per entry (dense: of 64 keys)
-  const int64_t scale_at = bh * ((a.cap + a.block - 1) / a.block);
+  const int64_t scale_at = bh * ((a.cap + a.block - 1) >> block_bits);
   int breg = -1, sreg = 0, lbase = 0;
   const int32_t* page_row = nullptr;
-  uint32_t head_of = 0;
+  int head_of = 0;
   if constexpr (F::PAGED) {
     const uint32_t seq = (uint32_t)bh / (uint32_t)a.heads;
-    head_of = (uint32_t)bh - seq * (uint32_t)a.heads;
+    head_of = (int)((uint32_t)bh - seq * (uint32_t)a.heads);
     page_row = a.pages + seq * a.n_table;
   }
   // (dense entries are 64 keys whatever the block size)
@@ -265,8 +272,10 @@ void cache_attn_kernel(typename F::Args a) {
     const int blk = b >> e_bits;
     if (b < 0 || blk >= n_blk) b = -1;
     if constexpr (F::PAGED) {
-      sreg = b < 0 ? -1 : page_row[blk];
-      if (sreg < 0 || sreg >= a.n_pages) b = -1, sreg = 0;
+      const int page = b < 0 ? -1 : page_row[blk];
+      if (page < 0 || page >= a.n_pages) b = -1;
+      // (dense: the entry's 64 keys of the page)
+      sreg = b < 0 ? 0 : (page * a.heads + head_of) * (a.block / C::KB) + (DENSE ? (b & ((1 << e_bits) - 1)) * SUB : 0);
     } else {
       sreg = 127 | 127 << 8;
       if (b >= 0) sreg = (int)a.k_scale[scale_at + blk] | (int)a.v_scale[scale_at + blk] << 8;
@@ -277,14 +286,14 @@ void cache_attn_kernel(typename F::Args a) {
   const int ntiles = cnt * SUB;
   struct Tile {
     int t;  // KB-key tile of the sequence, -1: none
-    int s;  // scale bytes, or the page
+    int s;  // scale bytes, or the tile's place in the pool, in tiles
   };
   auto fetch = [&](int j) -> Tile {
     if (j >= ntiles) return Tile{-1, F::PAGED ? 0 : 127 | 127 << 8};
     const int e = j / SUB;
     if (e >= lbase + 64) load_batch(lbase + 64);
     const int b = __builtin_amdgcn_readlane(breg, e - lbase);
-    return Tile{b < 0 ? -1 : b * SUB + j % SUB, __builtin_amdgcn_readlane(sreg, e - lbase)};
+    return Tile{b < 0 ? -1 : b * SUB + j % SUB, __builtin_amdgcn_readlane(sreg, e - lbase) + (F::PAGED ? j % SUB : 0)};
   };
 
   // ---- raw tiles: the lane's 16-code pieces at code src + 1024 i of a tile.  Each tile gets
@@ -295,9 +304,8 @@ void cache_attn_kernel(typename F::Args a) {
   auto load_raw = [&](const uint8_t* codes, const uint8_t* scales, Tile t, Piece (&u)[C::CV]) {
     const uint32_t n = (uint32_t)t.t < n_whole ? C::KB * D : ((uint32_t)t.t == n_whole ? last_codes : 0u);
     if constexpr (F::PAGED) {
-      // (tiles per page: a power of two)
-      const int64_t row = ((int64_t)t.s * a.heads + head_of) * a.block + (t.t & (a.block / C::KB - 1)) * C::KB;
-      const auto rs = tile_rsrc(codes + row * (D / 2), n / 2), rss = tile_rsrc(scales + row * (D / 32), n / 32);
+      const uint64_t at = (uint32_t)__builtin_amdgcn_readfirstlane(t.s);
+      const auto rs = tile_rsrc(codes + at * (C::KB * D / 2), n / 2), rss = tile_rsrc(scales + at * (C::KB * D / 32), n / 32);
 #pragma unroll
       for (int i = 0; i < C::CV; ++i) {
         u[i].u = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rs, src / 2 + 512 * i, 0, 0));

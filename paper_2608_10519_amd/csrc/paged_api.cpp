@@ -14,7 +14,8 @@ static int check_pages(const void* k, const void* v, const void* ks, const void*
     return report_error(SPARSTAR_ERR_INVALID_ARG, "n_table must be in [1, 2^30 / block_size]");
   if (n_pages < 1 || n_pages > INT32_MAX)
     return report_error(SPARSTAR_ERR_INVALID_ARG, "n_pages must be in [1, 2^31)");
-  if (n_pages * block_size > (int64_t(1) << 46) / (int64_t(H) * D))
+  // (the attention counts tiles of 4,096 values in 31 bits)
+  if (n_pages * block_size >= (int64_t(1) << 43) / (int64_t(H) * D))
     return report_error(SPARSTAR_ERR_INVALID_ARG, "cache too large");
   if (!k || !v || !ks || !vs || !pages)
     return report_error(SPARSTAR_ERR_INVALID_ARG, "the cache's four arrays and its pages must be non-null");
