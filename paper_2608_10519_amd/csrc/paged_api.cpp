@@ -110,7 +110,11 @@ extern "C" size_t sparstar_paged_attn_workspace_bytes(int B, int H, int64_t Lq, 
 extern "C" int sparstar_internal_paged_ranges(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                               int64_t kv_stride) {
   if (check_attn_sizes(B, H, Lq, Lk, D, block_size) != SPARSTAR_OK) return 1;
-  return paged_attn_plan(int64_t(B) * H, Lq, Lk, D, block_size, kv_stride, kv_stride == 0, true).ranges;
+  const bool dense = kv_stride == 0;
+  int most = 1;  // of lists of even and of uneven lengths
+  for (const bool uneven : {false, true})
+    most = std::max(most, paged_attn_plan(int64_t(B) * H, Lq, Lk, D, block_size, kv_stride, dense, true, uneven).ranges);
+  return most;
 }
 
 static int paged_attn_common(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
@@ -138,7 +142,8 @@ static int paged_attn_common(const void* q, const void* k_pages, const void* v_p
     return report_error(SPARSTAR_ERR_INVALID_ARG, "softmax_scale must be finite");
   const int64_t bh = int64_t(B) * H;
   const PagedPlan plan =
-      paged_attn_plan(bh, Lq, Lk, D, block_size, dense ? 0 : kv_stride, dense, workspace != nullptr);
+      paged_attn_plan(bh, Lq, Lk, D, block_size, dense ? 0 : kv_stride, dense, workspace != nullptr,
+                      !dense || (lens != nullptr && B > 1));
   if (paged_attn_threads(plan, bh * Lq, D) >= int64_t(1) << 32)
     return report_error(SPARSTAR_ERR_INVALID_ARG, "too many query rows and heads for one call");
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)

@@ -28,9 +28,9 @@ inline int paged_rows_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block)
 
 // More than 32 rows take the 8-bit cache's cut, whose ranges are a power of two, or such a number
 // of ranges that their work-groups fill the chip once, twice or three times and leave nothing
-// over, where the estimate finds that faster by 2% (calls of more than 200 us in few rounds: any number).  24
-// heads of 128 x 144,512 340 us in 16 ranges, 276 in 21; 18 of 220 x 10,061 59 us in 8, 44 in 14;
-// 24 of 64 x 144,512 187 us in 32, 175 in 42.
+// over, where the estimate finds that faster by 2% (calls of more than 200 us in few rounds: any
+// number).  24 heads of 128 x 144,512 302 us in 16 ranges, 271 in 21; 18 of 220 x 10,061 56 us in
+// 8, 44 in 14.
 inline CachePlan paged_rows_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
                                  bool may_split) {
   CachePlan p = cache_attn_plan(bh, lq, lk, d, block, kv_stride, dense, may_split);
@@ -54,6 +54,10 @@ inline CachePlan paged_rows_plan(int64_t bh, int64_t lq, int64_t lk, int d, int 
       if (const double t = time(int(r), w); t < best) best = t, ranges = int(r), rows = w;
     }
   }
+  // (a single group of rows reads the cache once, and what the chip then lacks is waves: 24 heads
+  // of 64 x 144,512 183 us in 32 ranges, 168 in 42; 64 x 40,000 61 and 58)
+  if (const int64_t r = 256 * 4 * kAttnWavesPerSimd * 32 / rows / bh; lq <= 64 && r > ranges && r <= most && nk >= 8 * r)
+    ranges = int(r);
   p.waves = rows / 32;
   p.ranges = ranges;
   const int64_t groups = (lq + rows - 1) / rows;
@@ -63,20 +67,37 @@ inline CachePlan paged_rows_plan(int64_t bh, int64_t lq, int64_t lk, int d, int 
   return p;
 }
 
-// Up to 32 rows stream the cache, in ranges of four waves each, two to a CU: more of them gain
-// nothing (24 heads of 144,512 rows 92 us with 504 work-groups, 100 with 240, 94 with 768), and
-// a wave reads four 64-key tiles at least.  A second launch that joins ranges costs what six
-// tiles of a lone wave cost (1.1 us each at D = 128), so lists of less than 48 tiles stay whole:
-// 24 heads of 4,000 rows 15.3 us in three ranges, 19.3 in one.  Where whole lists leave a CU to
-// one work-group it has eight waves (24 heads of 2,048 rows 12.1 us, 13.8 with four; 64 x 24
-// heads of 700 rows 51 and 36).
+// The time of a call of up to 32 rows in `ranges`, us: its start and, of more than one range, its
+// join; and the longer of a wave's tiles one after the other, with one work-group of four waves
+// (or one of eight, or two of four) on its CU, and of all codes and scales at 6.3 TB/s.
+// `uneven`: lists that may differ in length, of which the cut is by the longest.
+inline double paged_token_time_us(int64_t bh, int64_t lq, int d, int64_t tiles, int ranges, int waves, bool uneven) {
+  static constexpr double kTileUs[2][2][2] = {{{.82, 1.33}, {1.14, 1.83}}, {{1.2, 2.0}, {2.13, 3.17}}};
+  const bool two = bh * ranges > 256;
+  const double tile = kTileUs[d == 128][lq > 16][two || waves == 8];
+  const double memory = double(bh) * double(tiles) * 64 * (d + d / 16) / 6.3e6 * (uneven ? 0.85 : 1.0);
+  return (ranges > 1 ? 10.0 : 4.0) + (two && !uneven ? 1.5 : 0.0) + std::max(memory, tile * double(tiles) / (ranges * waves));
+}
+
+// Up to 32 rows stream the cache, in ranges of four waves each, which have a 64-key tile each at
+// least, and whose work-groups fill the chip once or twice; or whole, and where whole lists leave
+// a CU to one work-group it has eight waves (24 heads of 2,048 rows 12.1 us, 13.8 with four; 64 x
+// 24 heads of 700 rows 47 and 33).  One token, D = 128: 24 heads of 144,512 rows 78 us with 240
+// work-groups, 80 with 504; of 9,000 13.6 and 14.7; of 3,000 11.2 with 240, 15.9 whole; two
+// sequences of 24 heads, 84,032 rows each 88 us with 240 and 92 with 480, 84,032 and 67,226 87
+// and 84.  With 32 rows the matrix instructions want the second work-group: 24 heads of 144,512
+// rows 127 us and 97, as they do at D = 64: 2 x 24 heads of 84,032 rows 61 and 51.
 inline PagedPlan paged_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
-                                 bool may_split) {
+                                 bool may_split, bool uneven) {
   if (lq > 32) return PagedPlan{paged_rows_plan(bh, lq, lk, d, block, kv_stride, dense, may_split), 0};
   const int64_t nk = (lk + block - 1) / block, tiles = (dense ? nk : std::min(nk, kv_stride)) * (block / 64);
-  PagedPlan p{{1, 1, 0, 0, 0}, 4};
-  if (may_split && tiles >= 48) p.ranges = (int)std::min<int64_t>(paged_token_most_ranges(bh, lk, block), tiles / 16);
-  if (p.ranges == 1 && tiles > 8 && bh <= 256) p.token_waves = 8;
+  PagedPlan p{{1, 1, 0, 0, 0}, tiles > 8 && bh <= 256 ? 8 : 4};
+  double best = paged_token_time_us(bh, lq, d, tiles, 1, p.token_waves, uneven);
+  for (int fill = 256; may_split && fill <= 512; fill += 256) {
+    const int r = (int)std::min<int64_t>({fill / bh, tiles / 4, paged_token_most_ranges(bh, lk, block)});
+    if (r < 2) continue;
+    if (const double t = paged_token_time_us(bh, lq, d, tiles, r, 4, uneven); t < best) best = t, p.ranges = r, p.token_waves = 4;
+  }
   p.grid = bh * p.ranges;
   return p;
 }
