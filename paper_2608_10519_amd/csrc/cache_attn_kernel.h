@@ -136,10 +136,17 @@ __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, i
 // The softmax keeps a running max that is only refreshed when some lane's sum of a tile's
 // P exceeds 2^8 (attn_fwd.hip); the row sum of the bf16 P comes from 4x4x4 MFMAs.
 //
-// 24 dense heads of 2,880 x 75,392: 2.64 ms, 1.01 PFLOP/s, the matrix cores busy 52% of the
-// cycles at 1.83 GHz; 8 heads of 11,520 x 84,032 at 25%: 1.17 ms, 0.87 PFLOP/s (43%).  Beside
-// the bf16 forward, 24 heads: 25,920 x 98,432 dense 28.6 ms and 28.0, 11,520 x 84,032 at 25%
-// 3.54 and 3.23, 72,000 x 144,512 at 25% 34.1 and 33.3, and at 9.4%, block 128, 12.7 and 13.1.
+// D = 128, ms, all on one card (the clock differs between cards by some 3%):
+//                                          8 bits   4 bits   the bf16 forward
+//   24 heads,  2,880 x  75,392, dense       2.69     2.62     2.58
+//   24 heads, 25,920 x  98,432, dense      29.5     29.2     28.4
+//   24 heads, 11,520 x  84,032, 25%         3.45     3.34     3.25
+//   24 heads, 72,000 x 144,512, 25%        34.9     34.3     33.7
+//   24 heads, 72,000 x 144,512, 9.4%, 128  13.0     12.7     13.5
+//    8 heads, 11,520 x  84,032, 25%         1.18     1.16     1.13
+//    8 heads, 11,520 x  84,032, 25%, 128    1.05     1.02     1.03
+// The first is 1.02 PFLOP/s with 4 bits, the matrix cores busy half of the cycles at 1.8 GHz, the
+// VALU issuing 0.10 instructions per SIMD and cycle.
 template <int D, int NW>
 struct CachePipe : CacheCfg<D> {
   using B = CacheCfg<D>;

@@ -45,6 +45,10 @@ __device__ __forceinline__ uint32_t scale_byte_of(uint4 w) {
 
 // One thread per (K or V, token, chunk of 8 channels) and N heads, as rope_kernel; four
 // neighbouring threads share a scale.
+//
+// 24 heads, D = 128, keys rotated: 11,520 tokens 45 us with three heads a thread, 64 with one, 46
+// with two, 48 with four; 72,000 tokens 261 us (4.4 TB/s), 386, 271 and 257.  K's rotation in fp64
+// and the conversions share the time with memory: unrotated 38 us.
 template <bool INTERLEAVED, int N>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a) {
   const TokenChunk t = token_chunk((int64_t)a.b * a.l, a.l, a.d == 128 ? 4 : 3);

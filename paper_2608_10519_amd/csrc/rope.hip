@@ -3,7 +3,10 @@
 
 namespace sparstar {
 
-// One thread per pair and N rows, of which a work-group takes 256 / pairs at a time.
+// One thread per pair and N rows, of which a work-group takes 256 / pairs at a time.  16 rows a
+// thread read their coordinates side by side: 144,512 rows of 64 pairs 15.2 us (4.9 TB/s, all of
+// it writes), 27.1 with one row; with fewer than 8,192 work-groups of one row a thread those start
+// and end sooner (32,768 rows 7.5 and 6.5 us, 16,384 the same).
 //
 // The angle is taken in quarter turns, in fp64.  Adding 1.5 * 2^52 rounds it to a whole number n,
 // whose last bits are the sum's last bits, and leaves r in [-1/2, 1/2]: exact, so that a far
@@ -56,6 +59,12 @@ __global__ __launch_bounds__(256) void rope_table_kernel(RopeTableArgs a) {
 // first is turned: the table's entries (64 bytes a thread, against 48 for the chunk, its
 // partners' and its result) are read and made fp64 once.  A row lies in one wave, whose loads
 // of all of it come before its stores: y may be x.
+//
+// Memory bounds it.  24 heads, D = 128: 11,520 rows 29.5 us with three heads a thread (5.0 TB/s),
+// 34.9 with one, 29.8 with two, 29.2 with four; 72,000 rows 176 us (5.2 TB/s), 252, 189 and 173;
+// 3,000 rows 7.7 us, 9.7, 8.3 and 8.0.  Below some 8,192 rows of all heads three heads a thread
+// leave CUs without work, and the launch is all that counts.  Results go past the L2's share of
+// what is read (33 us without).
 template <bool INTERLEAVED, int N>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   const TokenChunk t = token_chunk((int64_t)a.b * a.l, a.l, a.d == 128 ? 4 : 3);
