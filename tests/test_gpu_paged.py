@@ -381,6 +381,26 @@ def test_many_heads(gpu_lib, Lq):
     check(o[pick], lse[pick], q[pick], c, pages[pick], None, [lens[b] for b in pick], 1 / math.sqrt(D))
 
 
+@pytest.mark.parametrize("Lq,block", [(1, 64), (7, 128), (64, 64)])
+def test_query_heads_that_share_keys(gpu_lib, Lq, block):
+    """Four query heads to a head of the cache are rows of one head; with lists where a head's rows
+    are whole blocks, or share one list."""
+    D, B, G, H, Lk = 128, 2, 4, 3, 500
+    g = torch.Generator().manual_seed(Lq)
+    n = -(-Lk // block)
+    c, pages = pool(gpu_lib, g, B * n, H, D, block), own_pages(g, B, n, B * n)
+    q = torch.randn(B, G * H, Lq, D, generator=g).bfloat16()
+    grouped = q.view(B, H, G * Lq, D)
+    one = [torch.randperm(n, generator=g)[: n // 2].sort().values.tolist() for _ in range(B * H)]
+    blocks = -(-G * Lq // block)
+    for lists in (None, [[[one[b * H + h]] * blocks for h in range(H)] for b in range(B)]):
+        o, lse = attend(gpu_lib, grouped.cuda(), c, pages.cuda(), lists, Lk, 0.1, None)
+        check(o, lse, grouped, c, pages, lists, [Lk] * B, 0.1)
+        for i in range(G):  # (each query head by itself: the same rows within the same tolerance)
+            alone, few = q.view(B, H, G, Lq, D)[:, :, i], lists and [[x[: -(-Lq // block)] for x in y] for y in lists]
+            check(o.view(B, H, G, Lq, D)[:, :, i], lse.view(B, H, G, Lq)[:, :, i], alone, c, pages, few, [Lk] * B, 0.1)
+
+
 @pytest.mark.parametrize("Lq", [1, 5, 130])
 def test_a_step_as_it_is_used(gpu_lib, Lq):
     """Rotation out of a fused projection, append, read for the selector, block-sparse attention:
