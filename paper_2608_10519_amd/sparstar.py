@@ -45,6 +45,9 @@ class Strides(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
 
 
+_strides = functools.lru_cache(maxsize=1024)(Strides)  # (made once per set of values; nothing changes them)
+
+
 def load(path: str | None = None) -> ctypes.CDLL:
     """Load the HIP library (once).  Raises if it is not built."""
     global _lib
@@ -593,7 +596,7 @@ def sparstar_rope_table(coords: torch.Tensor, freq: Sequence[float], axis: Seque
     if axis is not None and len(axis) != len(freq):
         raise ValueError("freq and axis differ in length")
     (rows, axes), pairs, dev = coords.shape, len(freq), coords.device
-    table = torch.empty((rows, pairs, 2), dtype=torch.float32, device=dev) if out is None else out
+    table = coords.new_empty((rows, pairs, 2), dtype=torch.float32) if out is None else out
     tp = _like(table, (rows, pairs, 2), torch.float32, "out", dev)
     f, ax = array.array("d", freq), array.array("i", axis) if axis is not None else None  # (held to the end of the call)
     _launch("sparstar_rope_table", dev, coords.data_ptr(), rows, axes, pairs, f.buffer_info()[0],
@@ -608,7 +611,7 @@ def _strided(t: torch.Tensor, name: str, device: torch.device | None = None, sha
         raise ValueError(f"{name} must be a 4-D bf16 tensor on the GPU [B, H, L, D] with contiguous rows")
     if device is not None and (t.device != device or t.shape != shape):
         raise ValueError(f"{name} must be a tensor on {device} of shape {tuple(shape)}")
-    return Strides(s[0], s[1], s[2])
+    return _strides(s[0], s[1], s[2])
 
 
 def _table(table: torch.Tensor, device: torch.device) -> tuple[int, int, int]:
@@ -625,7 +628,7 @@ def _rope(fn, x, table, start, positions, interleaved, out):
     tp, rows, pairs = _table(table, dev)
     pp = _like(positions, (B, L), torch.int32, "positions", dev)
     if out is None:
-        y, ys = torch.empty_like(x, memory_format=torch.contiguous_format), Strides(H * L * D, L * D, D)
+        y, ys = torch.empty_like(x, memory_format=torch.contiguous_format), _strides(H * L * D, L * D, D)
     else:
         y, ys = out, _strided(out, "out", dev, x.shape)
     _launch(fn, dev, x.data_ptr(), xs, B, H, L, D, tp, rows, pairs, int(interleaved), pp, start, y.data_ptr(), ys)
@@ -713,7 +716,7 @@ def sparstar_paged_read(cache: PagedCache, pages: torch.Tensor, start: int, L: i
     where, ptrs = _paged(cache, pages, B, H, D, dev)
     shape = (B, H, L, D)
     if out is None:
-        out = [torch.empty(shape, dtype=bf16, device=dev) if n in want else None for n in ("k", "v")]
+        out = [cache.k.new_empty(shape, dtype=bf16) if n in want else None for n in ("k", "v")]
         kp, vp = (t.data_ptr() if t is not None else None for t in out)
     else:
         kp, vp = _like(out[0], shape, bf16, "k", dev), _like(out[1], shape, bf16, "v", dev)
@@ -747,7 +750,7 @@ def _paged_attn(fn, q, cache, pages, lists, Lk, softmax_scale, lens, out, lse, r
     if lse is not None:
         lsep = _like(lse, (B, H, Lq), torch.float32, "lse", dev)
     elif return_lse:
-        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=dev)
+        lse = q.new_empty((B, H, Lq), dtype=torch.float32)
         lsep = lse.data_ptr()
     else:
         lsep = None
@@ -757,7 +760,7 @@ def _paged_attn(fn, q, cache, pages, lists, Lk, softmax_scale, lens, out, lse, r
             wp, wn = _scratch(workspace, dev)
         else:
             wn = _paged_scratch(B, H, Lq, Lk, D, b, listed[2] if listed else 0)
-            workspace = torch.empty(wn, dtype=torch.uint8, device=dev) if wn else None
+            workspace = q.new_empty(wn, dtype=torch.uint8) if wn else None
             wp = workspace.data_ptr() if wn else None
     _launch(fn, dev, q.data_ptr(), *ptrs, B, H, Lq, Lk, D, b, *where, lp, *listed, float(softmax_scale), op, lsep, wp, wn)
     return o, lse
