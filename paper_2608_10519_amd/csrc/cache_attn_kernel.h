@@ -228,6 +228,9 @@ void cache_attn_kernel(typename F::Args a) {
     qf[s] = __builtin_bit_cast(bf16x8, u);
   }
 
+  // (dense entries are 64 keys whatever the block size)
+  const int e_bits = DENSE ? (a.block == 128 ? 1 : 0) : 0;
+
   // ---- the range's key blocks: an even share of the list's entries, or of all blocks,
   // walked from `rot` on and around (see attn_fwd.hip for why)
   int first = 0, cnt, rot = 0;
@@ -240,6 +243,7 @@ void cache_attn_kernel(typename F::Args a) {
       n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
       list = a.kv_indices + r * a.stride;
     }
+    if constexpr (DENSE && F::PAGED) n <<= e_bits;
     // (a 64-bit division is some 150 scalar instructions)
     auto part = [&](int r) -> int {
       if (n < 1 << 25) return (int)((uint32_t)n * (uint32_t)r / (uint32_t)a.ranges);
@@ -263,9 +267,7 @@ void cache_attn_kernel(typename F::Args a) {
     head_of = (int)((uint32_t)bh - seq * (uint32_t)a.heads);
     page_row = a.pages + seq * a.n_table;
   }
-  // (dense entries are 64 keys whatever the block size)
-  const int e_bits = DENSE ? (a.block == 128 ? 1 : 0) : 0;
-  if constexpr (DENSE) {
+  if constexpr (DENSE && !F::PAGED) {  // (whole blocks, as the lists')
     first <<= e_bits;
     cnt <<= e_bits;
   }

@@ -18,52 +18,83 @@ inline int paged_token_most_ranges(int64_t bh, int64_t lk, int block) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({512 / bh, nk, kPagedMaxRanges}));
 }
 
-// The same of more rows: the 8-bit cache's, and beyond its 16 as many as fill the chip four times
-// with a wave per 32 rows, of two blocks at least.
+// The same of more rows: the 8-bit cache's, and as many as fill the chip three times with a wave
+// per 32 rows, of 64 keys at least.
 inline int paged_rows_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block) {
-  const int64_t nk = (lk + block - 1) / block, waves = bh * ((lq + 31) / 32);
-  const int base = cache_attn_most_ranges(bh, lq, lk, block);
-  return base < kSplits ? base : (int)std::max<int64_t>(base, std::min<int64_t>({4096 / std::max<int64_t>(waves, 1), nk / 2, 64}));
+  const int64_t waves = bh * ((lq + 31) / 32), filled = 3 * 256 * 4 * kAttnWavesPerSimd / std::max<int64_t>(waves, 1);
+  return (int)std::max<int64_t>(cache_attn_most_ranges(bh, lq, lk, block), std::min<int64_t>({filled, (lk + 63) / 64, 64}));
 }
 
-// More than 32 rows take the 8-bit cache's cut, whose ranges are a power of two, or such a number
-// of ranges that their work-groups fill the chip once, twice or three times and leave nothing
-// over, where the estimate finds that faster by 2% (calls of more than 200 us in few rounds: any
-// number).  24 heads of 128 x 144,512 302 us in 16 ranges, 271 in 21; 18 of 220 x 10,061 56 us in
-// 8, 44 in 14.
+// The time of a call of more than 32 rows whose lists hold `keys` keys, us: its start, the tiles
+// of work-groups that a CU holds one, two, three or four of (of two waves; of four: one or two),
+// round after round, and the join.  (Work-groups without work take places too: the last round of
+// two heads of 2,325 rows in 13 ranges starts 8 of 520, 49 us; in 12 ranges 39.)  Fitted to 450
+// random shapes of up to 250 us (1 to 72 heads, 33 to 6,000 x 200 to 140,000, dense and 5% to 65%,
+// both head dims and block sizes), each timed at some 13 cuts; the cut of the least estimate is
+// 0.7% slower than the best one on average, the 8-bit cache's cut 7% (up to 97%).
+inline double paged_rows_time_us(int64_t bh, int64_t lq, int64_t keys, int d, int ranges, int rows) {
+  static constexpr double kTileUs[2][2][4] = {{{.82, 1.17, 1.23, 1.32}, {.78, 1.18}}, {{.71, .95, 1.01, 1.09}, {.66, .95}}};
+  static constexpr double kStart[2][2] = {{.94, 1.3}, {.64, 1.7}};  // tiles that a work-group's start costs
+  const double* const us = kTileUs[d == 128][rows == 128];
+  const int per_cu = 4 * kAttnWavesPerSimd * 32 / rows;
+  const int64_t pairs = bh * ranges, groups = (lq + rows - 1) / rows, held = 32 * per_cu;
+  const int64_t an_xcd = (attn_grid(pairs, groups, attn_spread_bits(pairs, groups, rows)) + 7) / 8;
+  const int64_t whole = an_xcd / held, part = an_xcd - whole * held;
+  const double tiles = double(keys) / ranges / attn_tile_keys(d) + kStart[d == 128][rows == 128];
+  double t = 5.6 + double(whole) * tiles * us[per_cu - 1];
+  if (part > 0) t += tiles * us[(part + 31) / 32 - 1];
+  if (ranges > 1) t += 4.7 + 0.02 * ranges + double(bh) * double(lq) * ranges * (2 * d + 16) / 1.7e6;
+  return t;
+}
+
+// More than 32 rows take the cut of the least estimated time, among some numbers of ranges and
+// those that fill the chip once, twice or three times: 24 heads of 64 x 144,512 183 us in 32
+// ranges, 168 in 42; one head of 719 x 771 25 us whole, 12.5 in 12; 50 heads of 157 rows with lists of
+// 2,048 keys 52 us whole, 32 in 5.  Calls of more than 300 us, where the lists' shares of the L2
+// count, take the 8-bit cache's cut, or a number of ranges that fills the chip where the forward's
+// estimate finds that faster by 2%: 24 heads of 2,880 x 75,392 six ranges.
 inline CachePlan paged_rows_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
                                  bool may_split) {
-  CachePlan p = cache_attn_plan(bh, lq, lk, d, block, kv_stride, dense, may_split);
-  if (p.ranges == 1 && !may_split) return p;
-  const int64_t nk = (lk + block - 1) / block;
-  const int most = paged_rows_most_ranges(bh, lq, lk, block);
-  const bool full = dense || kv_stride >= nk;
-  const double rho = full ? 1.0 : double(kv_stride) / double(nk);
-  auto time = [&](int ranges, int rows) {
-    return attn_time_us(bh, lq, lk, d, block, rho, full, ranges, p.rotation > 0, rows);
-  };
-  double best = 0.98 * time(p.ranges, 32 * p.waves);
-  int ranges = p.ranges, rows = 32 * p.waves;
+  const int64_t nk = (lk + block - 1) / block, keys = dense ? lk : std::min(nk, kv_stride) * block;
+  const int64_t shares = dense ? (lk + 63) / 64 : std::min(nk, kv_stride);  // that a range can be made of
+  const int most = may_split ? paged_rows_most_ranges(bh, lq, lk, block) : 1;
+  CachePlan p{};
+  double best = 300.0;
   for (int w = dense ? 64 : block; w <= (dense ? 128 : block); w *= 2) {
     const int64_t items = bh * ((lq + w - 1) / w), held = 256 * 4 * kAttnWavesPerSimd * 32 / w;
-    const bool any = best > 200.0 && items <= 4 * held;
-    for (int i = 1; i <= (any ? most : 3); ++i) {
-      const int64_t r = any ? i : i * held / items;
-      if (r < 2 || r > most || nk < r) continue;
-      if (attn_grid(bh * r, (lq + w - 1) / w, 0) * 2 * w >> 32) break;  // launch limit
-      if (const double t = time(int(r), w); t < best) best = t, ranges = int(r), rows = w;
-    }
+    auto offer = [&](int64_t r) {
+      if (r < 1 || r > most || r > shares || (r > 1 && r * items > 3 * held)) return;
+      if (const double t = paged_rows_time_us(bh, lq, keys, d, int(r), w); t < best) best = t, p.ranges = int(r), p.waves = w / 32;
+    };
+    for (const int r : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) offer(r);
+    for (int i = 1; may_split && i <= 3; ++i) offer(i * held / items);
   }
-  // (a single group of rows reads the cache once, and what the chip then lacks is waves: 24 heads
-  // of 64 x 144,512 183 us in 32 ranges, 168 in 42; 64 x 40,000 61 and 58)
-  if (const int64_t r = 256 * 4 * kAttnWavesPerSimd * 32 / rows / bh; lq <= 64 && r > ranges && r <= most && nk >= 8 * r)
-    ranges = int(r);
-  p.waves = rows / 32;
-  p.ranges = ranges;
-  const int64_t groups = (lq + rows - 1) / rows;
-  p.spread_bits = attn_spread_bits(bh * ranges, groups, rows);
-  p.grid = attn_grid(bh * ranges, groups, p.spread_bits);
-  if (p.rotation > 0) p.rotation = 32 * 4 * kAttnWavesPerSimd / p.waves;
+  if (p.ranges == 0) {
+    p = cache_attn_plan(bh, lq, lk, d, block, kv_stride, dense, may_split);
+    const bool full = dense || kv_stride >= nk;
+    const double rho = full ? 1.0 : double(kv_stride) / double(nk);
+    auto time = [&](int ranges, int rows) {
+      return attn_time_us(bh, lq, lk, d, block, rho, full, ranges, p.rotation > 0, rows);
+    };
+    best = 0.98 * time(p.ranges, 32 * p.waves);
+    int ranges = p.ranges, rows = 32 * p.waves;
+    for (int w = dense ? 64 : block; may_split && w <= (dense ? 128 : block); w *= 2) {
+      const int64_t items = bh * ((lq + w - 1) / w), held = 256 * 4 * kAttnWavesPerSimd * 32 / w;
+      const bool any = items <= 4 * held;
+      for (int i = 1; i <= (any ? most : 3); ++i) {
+        const int64_t r = any ? i : i * held / items;
+        if (r < 2 || r > most || nk < r) continue;
+        if (attn_grid(bh * r, (lq + w - 1) / w, 0) * 2 * w >> 32) break;  // launch limit
+        if (const double t = time(int(r), w); t < best) best = t, ranges = int(r), rows = w;
+      }
+    }
+    p.waves = rows / 32;
+    p.ranges = ranges;
+    if (p.rotation > 0) p.rotation = 32 * 4 * kAttnWavesPerSimd / p.waves;
+  }
+  const int64_t groups = (lq + 32 * p.waves - 1) / (32 * p.waves);
+  p.spread_bits = attn_spread_bits(bh * p.ranges, groups, 32 * p.waves);
+  p.grid = attn_grid(bh * p.ranges, groups, p.spread_bits);
   return p;
 }
 
