@@ -543,9 +543,10 @@ int sparstar_rope_bwd(const void* dy, sparstar_strides dys, int B, int H, int64_
  *                      channel in the low half
  *   k_scale, v_scale   [n_pages, H, block_size, D / 32] bytes e + 127, one for 32 channels of
  *                      a token
- * (all 16-byte aligned, less than 2^43 values), and a value is code * 2^e with e in [-125, 125]: exact in bf16.  A code
- * stands for 0, 1/2, 1, 3/2, 2, 3, 4 or 6 (0..7), negated in 8..15.  Scale byte 255 makes its
- * 32 values NaN.  Row r of sequence b is row r % block_size of page
+ * (all 16-byte aligned, less than 2^43 values), and a value is code * 2^e with e in
+ * [-125, 125]: exact in bf16.  A code stands for 0, 1/2, 1, 3/2, 2, 3, 4 or 6 (0..7), negated
+ * in 8..15.  Scale byte 255 makes its 32 values NaN.  Row r of sequence b is row
+ * r % block_size of page
  *   pages[b, r / block_size]     device int32 [B, n_table]
  * A page may stand in the tables of several sequences, which then share its rows.  One
  * outside [0, n_pages) does not exist: what would be written there is dropped, it reads as

@@ -326,7 +326,8 @@ def test_offsets_past_32_bits(gpu_lib, Lq):
 
 JOINS = [  # D, block, H, Lq, Lk, list length (0: dense), ranges
     (128, 64, 1, 1, 9000, 0, 35), (64, 128, 2, 7, 9000, 30, 15), (128, 128, 3, 32, 14_000, 0, 55), (64, 64, 2, 17, 9000, 60, 15),
-    (64, 64, 85, 1, 5000, 0, 6),
+    (64, 64, 85, 1, 5000, 0, 6), (128, 128, 3, 54, 1724, 0, None), (64, 128, 2, 100, 1100, 0, None), (128, 64, 2, 97, 738, 0, None),
+    (128, 128, 4, 130, 2500, 13, None),
     (128, 128, 1, 100, 9000, 0, None), (64, 64, 1, 64, 9000, 60, None), (128, 64, 18, 220, 3500, 0, None),
     (64, 64, 3, 300, 9000, 0, None),
 ]
