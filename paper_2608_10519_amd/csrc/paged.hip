@@ -43,14 +43,34 @@ __device__ __forceinline__ uint32_t scale_byte_of(uint4 w) {
   return nan ? kPagedNan : (uint32_t)min(max(byte, kPagedExpMin + 127), kPagedExpMax + 127);
 }
 
+// A 4 x 4 transposition among four neighbouring threads: thread i gets every thread's w[i], by
+// two exchanges of the half that the other needs.
+__device__ __forceinline__ uint4 transposed(const uint32_t (&w)[4], int i) {
+  auto from = [](uint32_t x, auto perm) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, perm(), 15, 15, true);
+  };
+  auto next = [] { return 0xb1; };    // lanes 1 0 3 2
+  auto second = [] { return 0x4e; };  // lanes 2 3 0 1
+  const bool odd = i & 1, high = i & 2;
+  const uint32_t a = from(odd ? w[0] : w[1], next), b = from(odd ? w[2] : w[3], next);
+  const uint2 lo = odd ? make_uint2(a, w[1]) : make_uint2(w[0], a);  // this pair's of i % 2
+  const uint2 hi = odd ? make_uint2(b, w[3]) : make_uint2(w[2], b);  // and of i % 2 + 2
+  const uint2 give = high ? lo : hi;
+  const uint2 got = make_uint2(from(give.x, second), from(give.y, second));
+  return high ? make_uint4(got.x, got.y, hi.x, hi.y) : make_uint4(lo.x, lo.y, got.x, got.y);
+}
+
 // One thread per (K or V, token, chunk of 8 channels) and N heads, as rope_kernel; four
-// neighbouring threads share a scale.
+// neighbouring threads share a scale.  With four heads each of the four stores one head's codes
+// and scale, 16 bytes in place of four.
 //
-// 24 heads, D = 128, keys rotated: 11,520 tokens 45 us with three heads a thread, 64 with one, 46
-// with two, 48 with four; 72,000 tokens 261 us (4.4 TB/s), 386, 271 and 257.  K's rotation in fp64
-// and the conversions share the time with memory: unrotated 38 us.
+// 24 heads, D = 128, keys rotated: 11,520 tokens 42 us (4.4 TB/s), 64 with one head a thread;
+// 72,000 tokens 232 us (5.0 TB/s), 386; 500 tokens 5.2 and 5.5, 340 4.0 both, 170 3.9 and 3.6 (in
+// a captured graph).  Three heads a thread, each storing its own codes: 43 and 247.  Unrotated 36 and 208: K's rotation in fp64 is what memory does not hide.  Stores past
+// the caches write 11,520 tokens in 39 us, but a read of them takes 44 then, 27 now.
 template <bool INTERLEAVED, int N>
 __global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a) {
+  static_assert(N == 1 || N == 4);
   const TokenChunk t = token_chunk((int64_t)a.b * a.l, a.l, a.d == 128 ? 4 : 3);
   if (!t.ok) return;  // (whole rows of threads: whole groups of four)
   // (K and V in turn: the turns' work lies beside V's loads)
@@ -69,7 +89,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a) {
   const Strides& s = is_v ? a.vs : a.ks;
   const uint16_t* x = (is_v ? a.v : a.k) + t.b * s.b + t.l * s.l + h0 * s.h;
   const int64_t at_row = ((page * a.heads + h0) << block_bits) + (row & (a.block - 1));
-  uint8_t* const codes = (is_v ? a.v_pages : a.k_pages) + at_row * (a.d / 2) + 4 * c;
+  uint8_t* const codes = (is_v ? a.v_pages : a.k_pages) + at_row * (a.d / 2);
   uint8_t* const scale = (is_v ? a.v_scale : a.k_scale) + at_row * (a.d / 32) + c / 4;
   uint4 own[N], other[N];
 #pragma unroll
@@ -78,20 +98,29 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a) {
     own[h] = *reinterpret_cast<const uint4*>(x + h * s.h + 8 * c);
     if (!INTERLEAVED && u.other >= 0) other[h] = *reinterpret_cast<const uint4*>(x + h * s.h + u.other);
   }
+  uint32_t code[N], byte[N];
 #pragma unroll
   for (int h = 0; h < N; ++h) {
+    code[h] = byte[h] = 0;
     if (h >= left) continue;
     const uint4 w = u.other >= 0 ? turned(u, own[h], INTERLEAVED ? own[h] : other[h], INTERLEAVED) : own[h];
-    const uint32_t byte = scale_byte_of(w);
+    byte[h] = scale_byte_of(w);
     // (the conversion divides by the scale, rounds to the nearest, ties to even, and saturates)
-    const float sc = __uint_as_float(byte << 23);
-    uint32_t r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.x), sc, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.y), sc, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.z), sc, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w.w), sc, 3);
-    *reinterpret_cast<uint32_t*>(codes + h * (a.block * (a.d / 2))) = r;
-    if (c % 4 == 0) scale[h * (a.block * (a.d / 32))] = (uint8_t)byte;
+    const float sc = __uint_as_float(byte[h] << 23);
+    code[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code[h], __builtin_bit_cast(bf16x2, w.x), sc, 0);
+    code[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code[h], __builtin_bit_cast(bf16x2, w.y), sc, 1);
+    code[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code[h], __builtin_bit_cast(bf16x2, w.z), sc, 2);
+    code[h] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code[h], __builtin_bit_cast(bf16x2, w.w), sc, 3);
+  }
+  if constexpr (N == 4) {
+    const int h = c % 4;
+    const uint4 w = transposed(code, h);
+    if (h >= left) return;
+    *reinterpret_cast<uint4*>(codes + h * (a.block * (a.d / 2)) + 16 * (c / 4)) = w;
+    scale[h * (a.block * (a.d / 32))] = (uint8_t)(h == 0 ? byte[0] : h == 1 ? byte[1] : h == 2 ? byte[2] : byte[3]);
+  } else {
+    *reinterpret_cast<uint32_t*>(codes + 4 * c) = code[0];
+    if (c % 4 == 0) *scale = (uint8_t)byte[0];
   }
 }
 
@@ -152,7 +181,7 @@ static hipError_t launch_writes(const PagedArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_write(const PagedArgs& a, hipStream_t stream) {
-  return (int64_t)a.b * a.heads * a.l >= 8192 ? launch_writes<3>(a, stream) : launch_writes<1>(a, stream);
+  return (int64_t)a.b * a.heads * a.l >= 8192 ? launch_writes<4>(a, stream) : launch_writes<1>(a, stream);
 }
 
 template <int CPR, int W, int P, bool ONCE>

@@ -63,8 +63,9 @@ __global__ __launch_bounds__(256) void rope_table_kernel(RopeTableArgs a) {
 // Memory bounds it.  24 heads, D = 128: 11,520 rows 29.5 us with three heads a thread (5.0 TB/s),
 // 34.9 with one, 29.8 with two, 29.2 with four; 72,000 rows 176 us (5.2 TB/s), 252, 189 and 173;
 // 3,000 rows 7.7 us, 9.7, 8.3 and 8.0.  Below some 8,192 rows of all heads three heads a thread
-// leave CUs without work, and the launch is all that counts.  Results go past the L2's share of
-// what is read (33 us without).
+// leave CUs without work: 340 rows 3.3 us with one and 3.1 with three, 170 2.8 and 3.0, 64 2.4
+// and 2.9 (in a captured graph, without the calls' own time).  Results go past
+// the L2's share of what is read (11,520 rows 33 us without).
 template <bool INTERLEAVED, int N>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   const TokenChunk t = token_chunk((int64_t)a.b * a.l, a.l, a.d == 128 ? 4 : 3);
