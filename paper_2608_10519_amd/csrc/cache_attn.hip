@@ -302,7 +302,7 @@ static hipError_t launch_mode(const CacheAttnArgs& a, int waves, hipStream_t str
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return launch_merge<D, 16, Codes8>(a, stream);
   }
-  return launch_rows<D, DENSE, Codes8>(a, waves, stream);
+  return launch_rows<D, DENSE, Codes8>(a, waves, cache_join_groups(waves, (int64_t)a.bh * a.lq, a.ranges), stream);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int d, int waves, bool dense, hipStream_t stream) {

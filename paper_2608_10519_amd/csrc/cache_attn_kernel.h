@@ -602,8 +602,8 @@ void cache_attn_kernel(typename F::Args a) {
 // Joins the ranges of one row: with M = max_r m_r and w_r = 2^(m_r - M),
 // O = sum w_r 2^e_r A_r / sum w_r l_r and lse = ln 2 (M + log2 sum w_r le_r).  D / 8 threads
 // per row and G groups of them, each over every G-th range; the groups' own sums are joined
-// the same way through LDS.  16 groups suit few rows (one head of 100 x 3,000: 14.9 us, 19.3
-// with one), one group many (8 heads of 11,520 x 84,032: 1.18 ms, 1.26 with 16).
+// the same way through LDS.  Groups suit many ranges of few rows, one group many rows (64 rows
+// in 64 ranges 4.0 us with 16 groups, 16.5 with one; 14,400 in 8 19 and 7.4).
 template <int D, int G, class F>
 __global__ __launch_bounds__(256) void cache_merge_kernel(typename F::Args a) {
   constexpr int LPR = D / 8, RPB = 256 / (LPR * G);
@@ -613,19 +613,29 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(typename F::Args a) {
   const bool ok = row < rows;
   float m = -INFINITY, l = 0.f, le = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (ok) {
-#pragma unroll 4
-    for (int r = g; r < a.ranges; r += G) {
-      const int64_t p = (int64_t)r * rows + row;
-      const float4 x = reinterpret_cast<const float4*>(a.part_meta)[p];
-      const f16x8 u = *reinterpret_cast<const f16x8*>(reinterpret_cast<const _Float16*>(a.part_o) + p * D + 8 * c);
-      if (x.y == 0.f) continue;  // no key seen; NaN passes on
-      const float mn = fmaxf(m, x.x), s = __builtin_amdgcn_exp2f(m - mn), t = __builtin_amdgcn_exp2f(x.x - mn);
-      const float w = __builtin_amdgcn_ldexpf(t, (int)x.w);
-      l = l * s + x.y * t;
-      le = le * s + x.z * t;
+    // (four ranges' loads at once: with one after the other their latency was half of the time)
+    for (int r0 = 0; r0 < a.ranges; r0 += 4 * G) {
+      float4 x[4];
+      f16x8 u[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, (float)u[e], acc[e] * s);
-      m = mn;
+      for (int i = 0; i < 4; ++i) {
+        x[i] = make_float4(0.f, 0.f, 0.f, 0.f), u[i] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (r0 + i * G >= a.ranges) continue;
+        const int64_t p = (int64_t)min(r0 + i * G + g, a.ranges - 1) * rows + row;
+        x[i] = reinterpret_cast<const float4*>(a.part_meta)[p];
+        u[i] = *reinterpret_cast<const f16x8*>(reinterpret_cast<const _Float16*>(a.part_o) + p * D + 8 * c);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (r0 + i * G + g >= a.ranges || x[i].y == 0.f) continue;  // no key seen; NaN passes on
+        const float mn = fmaxf(m, x[i].x), s = __builtin_amdgcn_exp2f(m - mn), t = __builtin_amdgcn_exp2f(x[i].x - mn);
+        const float w = __builtin_amdgcn_ldexpf(t, (int)x[i].w);
+        l = l * s + x[i].y * t;
+        le = le * s + x[i].z * t;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, (float)u[i][e], acc[e] * s);
+        m = mn;
+      }
     }
   }
   if constexpr (G > 1) {
@@ -671,12 +681,14 @@ static hipError_t launch_merge(const typename F::Args& a, hipStream_t stream) {
 
 // The launches of a call of more than 32 rows.
 template <int D, bool DENSE, class F>
-static hipError_t launch_rows(const typename F::Args& a, int waves, hipStream_t stream) {
+static hipError_t launch_rows(const typename F::Args& a, int waves, int join_groups, hipStream_t stream) {
   if (waves == 2) cache_attn_kernel<D, 2, DENSE, F><<<a.grid, 128, 0, stream>>>(a);
   else cache_attn_kernel<D, 4, DENSE, F><<<a.grid, 256, 0, stream>>>(a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  return cache_join_groups(waves, (int64_t)a.bh * a.lq, a.ranges) > 1 ? launch_merge<D, 16, F>(a, stream)
-                                                                      : launch_merge<D, 1, F>(a, stream);
+  if constexpr (F::PAGED) {
+    if (join_groups == 4) return launch_merge<D, 4, F>(a, stream);
+  }
+  return join_groups > 1 ? launch_merge<D, 16, F>(a, stream) : launch_merge<D, 1, F>(a, stream);
 }
 
 }  // namespace sparstar

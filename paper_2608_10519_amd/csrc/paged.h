@@ -68,6 +68,7 @@ struct PagedAttnArgs : CacheAttnArgs {
   int64_t n_table, n_pages;
   float* part32;                   // up to 32 rows: fp32 partial results [ranges, BH, Lq, D]
   int waves, token_waves;          // of a work-group (launcher only), as in PagedPlan
+  int join_groups;                 // (launcher only, more than 32 rows)
 };
 
 hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t stream);

@@ -180,6 +180,7 @@ static int paged_attn_common(const void* q, const void* k_pages, const void* v_p
   a.grid = plan.grid;
   a.waves = plan.waves;
   a.token_waves = plan.token_waves;
+  a.join_groups = paged_join_groups(bh * Lq, D, plan.ranges);
   if (plan.ranges > 1) {
     a.part_o = static_cast<uint16_t*>(workspace);  // (more than 32 rows)
     a.part32 = static_cast<float*>(workspace);

@@ -358,17 +358,27 @@ __global__ __launch_bounds__(D / 4 * G) void paged_join_kernel(PagedAttnArgs a) 
   const int64_t rows = (int64_t)a.bh * a.lq, row = blockIdx.x;
   float m = -INFINITY, l = 0.f, le = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int r = g; r < a.ranges; r += G) {
-    const int64_t p = (int64_t)r * rows + row;
-    const float4 y = reinterpret_cast<const float4*>(a.part_meta)[p];
-    const float4 u = *reinterpret_cast<const float4*>(a.part32 + p * D + 4 * c);
-    if (y.y == 0.f) continue;  // no key seen; NaN passes on
-    const float mn = fmaxf(m, y.x), s = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    const float t = y.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(y.x - mn);
-    l = fmaf(l, s, y.y * t), le = fmaf(le, s, y.z * t);
-    x.x = fmaf(u.x, t, x.x * s), x.y = fmaf(u.y, t, x.y * s), x.z = fmaf(u.z, t, x.z * s), x.w = fmaf(u.w, t, x.w * s);
-    m = mn;
+  // (kPagedMaxRanges are four a thread: all loads at once)
+  for (int r0 = 0; r0 < a.ranges; r0 += 4 * G) {
+    float4 y[4], u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[i] = u[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r0 + i * G >= a.ranges) continue;
+      const int64_t p = (int64_t)min(r0 + i * G + g, a.ranges - 1) * rows + row;
+      y[i] = reinterpret_cast<const float4*>(a.part_meta)[p];
+      u[i] = *reinterpret_cast<const float4*>(a.part32 + p * D + 4 * c);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (r0 + i * G + g >= a.ranges || y[i].y == 0.f) continue;  // no key seen; NaN passes on
+      const float mn = fmaxf(m, y[i].x), s = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float t = y[i].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(y[i].x - mn);
+      l = fmaf(l, s, y[i].y * t), le = fmaf(le, s, y[i].z * t);
+      x.x = fmaf(u[i].x, t, x.x * s), x.y = fmaf(u[i].y, t, x.y * s);
+      x.z = fmaf(u[i].z, t, x.z * s), x.w = fmaf(u[i].w, t, x.w * s);
+      m = mn;
+    }
   }
   red[g][c] = x;
   if (c == 0) meta[g][0] = m, meta[g][1] = l, meta[g][2] = le;
@@ -404,7 +414,7 @@ static hipError_t launch_token(const PagedAttnArgs& a, hipStream_t stream) {
 
 template <int D, bool DENSE>
 static hipError_t launch_mode(const PagedAttnArgs& a, hipStream_t stream) {
-  if (a.waves > 1) return launch_rows<D, DENSE, Codes4>(a, a.waves, stream);
+  if (a.waves > 1) return launch_rows<D, DENSE, Codes4>(a, a.waves, a.join_groups, stream);
   const hipError_t e = a.token_waves == 8 ? launch_token<D, DENSE, 8>(a, stream) : launch_token<D, DENSE, 4>(a, stream);
   if (e != hipSuccess || a.ranges == 1) return e;
   paged_join_kernel<D, kJoinGroups><<<(int64_t)a.bh * a.lq, D / 4 * kJoinGroups, 0, stream>>>(a);

@@ -30,8 +30,8 @@ inline int paged_rows_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block)
 // round after round, and the join.  (Work-groups without work take places too: the last round of
 // two heads of 2,325 rows in 13 ranges starts 8 of 520, 49 us; in 12 ranges 39.)  Fitted to 450
 // random shapes of up to 250 us (1 to 72 heads, 33 to 6,000 x 200 to 140,000, dense and 5% to 65%,
-// both head dims and block sizes), each timed at some 13 cuts; the cut of the least estimate is
-// 0.7% slower than the best one on average, the 8-bit cache's cut 7% (up to 97%).
+// both head dims and block sizes), each timed at some 13 cuts; on 500 others the cut of the least
+// estimate is 0.8% slower than the best one on average, the 8-bit cache's cut 7% (up to 97%).
 inline double paged_rows_time_us(int64_t bh, int64_t lq, int64_t keys, int d, int ranges, int rows) {
   static constexpr double kTileUs[2][2][4] = {{{.82, 1.17, 1.23, 1.32}, {.78, 1.18}}, {{.71, .95, 1.01, 1.09}, {.66, .95}}};
   static constexpr double kStart[2][2] = {{.94, 1.3}, {.64, 1.7}};  // tiles that a work-group's start costs
@@ -142,10 +142,20 @@ inline size_t paged_attn_workspace(int64_t bh, int64_t lq, int64_t lk, int d, in
   return ranges > 1 ? paged_part_bytes(bh * lq, lq, d, ranges) + size_t(bh * lq) * ranges * 4 * sizeof(float) : 0;
 }
 
+// Groups of threads that share the join of a row's ranges (cache_merge_kernel; a thread loads four
+// ranges at a time).  D = 128, us in one, 4 and 16 groups: 64 rows in 16 ranges 5.2, 3.9, 3.9, in 64
+// 16.5, 6.4, 4.0; 2,400 in 8 3.9, 4.0, 5.1, in 16 5.5, 4.6, 6.0, in 64 16.9, 9.1, 11.4; 7,200 in 16
+// 7.4, 7.8, 12.3, in 64 21.6, 21.8, 27.5.
+inline int paged_join_groups(int64_t rows, int d, int ranges) {
+  if (ranges <= 8 || rows * d >= 5000 * 128) return 1;
+  return ranges > 16 && rows * d <= 1000 * 128 ? 16 : 4;
+}
+
 // Threads of the largest launch of a call, of which there may be fewer than 2^32.
 inline int64_t paged_attn_threads(const PagedPlan& p, int64_t rows, int d) {
-  if (p.waves > 1) return cache_attn_threads(p, rows, d);
-  return std::max<int64_t>(p.grid * 64 * p.token_waves, p.ranges > 1 ? rows * d * 4 : 0);
+  if (p.waves == 1) return std::max<int64_t>(p.grid * 64 * p.token_waves, p.ranges > 1 ? rows * d * 4 : 0);
+  const int64_t join = p.ranges > 1 ? rows * (d / 8) * paged_join_groups(rows, d, p.ranges) + 256 : 0;
+  return std::max(p.grid * 64 * p.waves, join);
 }
 
 }  // namespace sparstar
