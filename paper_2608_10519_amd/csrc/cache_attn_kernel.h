@@ -209,11 +209,11 @@ void cache_attn_kernel(typename F::Args a) {
   const int l32 = lane % 32, hh = lane / 32;
 
   // tokens that exist: rows past them are neither read nor attended to
-  int64_t len = a.lk;
-  if (a.lens != nullptr) {
-    const int n = a.lens[(uint32_t)bh / (uint32_t)a.heads];
-    len = n < 0 ? 0 : (n < a.lk ? n : a.lk);
-  }
+  // (both counts are loaded before either is waited for)
+  int given = 0, listed = 0;
+  if (a.lens != nullptr) given = a.lens[(uint32_t)bh / (uint32_t)a.heads];
+  if constexpr (!DENSE) listed = a.kv_num_blocks[bh * a.n_q + qg];
+  const int64_t len = a.lens == nullptr ? a.lk : (given < 0 ? 0 : (given < a.lk ? given : a.lk));
   const int block_bits = a.block == 128 ? 7 : 6;
   const int n_blk = (int)((len + a.block - 1) >> block_bits);
 
@@ -238,10 +238,8 @@ void cache_attn_kernel(typename F::Args a) {
   {
     int n = n_blk;
     if constexpr (!DENSE) {
-      const int64_t r = bh * a.n_q + qg;
-      n = a.kv_num_blocks[r];
-      n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
-      list = a.kv_indices + r * a.stride;
+      n = listed < 0 ? 0 : (listed > a.stride ? a.stride : listed);
+      list = a.kv_indices + (bh * a.n_q + qg) * a.stride;
     }
     if constexpr (DENSE && F::PAGED) n <<= e_bits;
     // (a 64-bit division is some 150 scalar instructions)

@@ -54,11 +54,11 @@ void paged_token_kernel(PagedAttnArgs a) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int l16 = lane % 16, j = lane / 16;
 
-  int64_t len = a.lk;
-  if (a.lens != nullptr) {
-    const int n = a.lens[b];
-    len = n < 0 ? 0 : (n < a.lk ? n : a.lk);
-  }
+  // (both counts are loaded before either is waited for)
+  int given = 0, listed = 0;
+  if (a.lens != nullptr) given = a.lens[b];
+  if constexpr (!DENSE) listed = a.kv_num_blocks[bh];  // (one query block)
+  const int64_t len = a.lens == nullptr ? a.lk : (given < 0 ? 0 : (given < a.lk ? given : a.lk));
   const int sub_bits = a.block == 128 ? 1 : 0;
   const int n_blk = (int)((len + a.block - 1) >> (6 + sub_bits));
 
@@ -80,8 +80,7 @@ void paged_token_kernel(PagedAttnArgs a) {
   {
     int n = n_blk;
     if constexpr (!DENSE) {
-      n = a.kv_num_blocks[bh];  // (one query block)
-      n = n < 0 ? 0 : (n > a.stride ? a.stride : n);
+      n = listed < 0 ? 0 : (listed > a.stride ? a.stride : listed);
       list = a.kv_indices + bh * a.stride;
     }
     const uint32_t part = range * W + wave, parts = a.ranges * W, all = (uint32_t)n << sub_bits;
