@@ -71,6 +71,25 @@ struct PagedAttnArgs : CacheAttnArgs {
   int join_groups;                 // (launcher only, more than 32 rows)
 };
 
+// Work-groups are launched in rows of at most 2^20: a launch may have fewer than 2^32 threads
+// along each axis.  (The last row's may be more than there is work for.)
+inline dim3 rows_of_groups(int64_t n) {
+  constexpr int64_t kRow = 1 << 20;
+  const int64_t rows = (n + kRow - 1) / kRow;
+  return dim3((uint32_t)((n + rows - 1) / rows), (uint32_t)rows);
+}
+
+// What work-group w of a read has to do: the first n take K where it is wanted, the next n (or
+// the first) V where that is, and those that only fill the last row of the grid nothing.
+struct ReadGroup {
+  int64_t at;
+  bool is_v, any;
+};
+constexpr ReadGroup read_group(int64_t w, int64_t n, bool want_k, bool want_v) {
+  const bool is_v = !want_k || w >= n;
+  return ReadGroup{want_k && is_v ? w - n : w, is_v, w < n * (int(want_k) + int(want_v))};
+}
+
 hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t stream);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 hipError_t launch_paged_write(const PagedArgs& a, hipStream_t stream);

@@ -129,11 +129,11 @@ __global__ __launch_bounds__(256) void paged_write_kernel(PagedArgs a) {
 template <int CPR, int W, int P, bool ONCE>
 __global__ __launch_bounds__(256) void paged_read_kernel(PagedArgs a) {
   constexpr int TPR = CPR / W, RPP = 256 / TPR;
-  const int64_t per = (a.l + RPP * P - 1) / (RPP * P), n = (int64_t)a.b * a.heads * per, w0 = group_of_rows();
-  // the first n work-groups take K where it is wanted, the next n (or the first) V
-  const bool is_v = a.k_out == nullptr || w0 >= n;
-  const int64_t w = a.k_out != nullptr && is_v ? w0 - n : w0;
-  if (w >= n) return;
+  const int64_t per = (a.l + RPP * P - 1) / (RPP * P), n = (int64_t)a.b * a.heads * per;
+  const ReadGroup group = read_group(group_of_rows(), n, a.k_out != nullptr, a.v_out != nullptr);
+  if (!group.any) return;
+  const bool is_v = group.is_v;
+  const int64_t w = group.at;
   const int64_t bh = divide(w, per), b = divide(bh, a.heads), h = bh - b * a.heads;
   const int64_t l0 = (w - bh * per) * (RPP * P) + threadIdx.x / TPR;
   const int c = threadIdx.x % TPR, block_bits = a.block == 128 ? 7 : 6;

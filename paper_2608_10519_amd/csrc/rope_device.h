@@ -80,13 +80,6 @@ __device__ __forceinline__ void store_once(uint16_t* p, uint4 r) {
   __builtin_nontemporal_store((u32x4){r.x, r.y, r.z, r.w}, reinterpret_cast<u32x4*>(p));
 }
 
-// Work-groups are launched in rows of at most 2^20: a launch may have fewer than 2^32 threads
-// along each axis.
-inline dim3 rows_of_groups(int64_t n) {
-  constexpr int64_t kRow = 1 << 20;
-  const int64_t rows = (n + kRow - 1) / kRow;
-  return dim3((uint32_t)((n + rows - 1) / rows), (uint32_t)rows);
-}
 __device__ __forceinline__ int64_t group_of_rows() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // a / b of numbers that mostly fit 32 bits, where a division takes a fifth of the instructions.
