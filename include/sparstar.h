@@ -602,8 +602,8 @@ size_t sparstar_paged_attn_workspace_bytes(int B, int H, int64_t Lq, int64_t Lk,
  * 8-bit cache's calls, but for
  *   pages, n_table  device int32 [B, n_table], Lk <= n_table * block_size
  *   kv_stride       at most 2^28
- *   workspace       of sparstar_paged_attn_workspace_bytes(...) bytes; up to 32 query rows
- *                   the ranges' sums are kept in fp32 there, of more rows in fp16 as there.
+ *   workspace       of sparstar_paged_attn_workspace_bytes(...) bytes; the ranges' sums are
+ *                   kept in fp32 there, so that a cut adds no rounding to fewer bits.
  */
 int sparstar_paged_sparse_attn_fwd(const void* q, const void* k_pages, const void* v_pages, const uint8_t* k_scale,
                                    const uint8_t* v_scale, int B, int H, int64_t Lq, int64_t Lk, int D,

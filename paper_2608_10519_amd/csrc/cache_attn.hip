@@ -292,7 +292,7 @@ void cache_token_kernel(CacheAttnArgs a) {
       x[e + 2] = fmaf(u.z, f, x[e + 2]), x[e + 3] = fmaf(u.w, f, x[e + 3]);
     }
   }
-  store_rows<D>(a, bh, row, range, acc, m, l, le, hh);
+  store_rows<D, Codes8>(a, bh, row, range, acc, m, l, le, hh);
 }
 
 template <int D, bool DENSE>

@@ -37,6 +37,7 @@ __device__ __forceinline__ bf16x8 decode8(uint2 u, float scale) {
 // 8 bits: e4m3 codes [BH, cap, D], a scale byte per block.
 struct Codes8 {
   using Args = CacheAttnArgs;
+  using Part = f16x8;  // of a range's P V (store_rows)
   static constexpr bool PAGED = false;
   static constexpr int BITS = 8;
   struct Piece {
@@ -48,6 +49,7 @@ struct Codes8 {
 // 32 channels.
 struct Codes4 {
   using Args = PagedAttnArgs;
+  using Part = f32x8;
   static constexpr bool PAGED = true;
   static constexpr int BITS = 4;
   struct Piece {
@@ -67,17 +69,21 @@ __device__ __forceinline__ bf16x8 decode8_4bit(uint32_t u, float scale) {
 }
 
 // Writes the lane's query row (its columns 32 t + 8 g + 4 h + 0..3): O and lse, or, with
-// several ranges, the range's unnormalised P V in fp16 with the running max (log2 units),
-// the two row sums and the exponent of the scale.  fp16 rounds once more, by at most 2^-11
-// of the value, an eighth of what P's rounding to bf16 may change, for half the bytes of
-// fp32.  The scale, a power of two, brings the row's largest magnitude to [2^14, 2^15), the
-// top of fp16's range, so that a column down to 2^-28 of it keeps all 11 bits.  m, l and le
-// are the row's; l == 0 means no key was seen (a NaN passes on).
-template <int D>
-__device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, int64_t row, int range,
+// several ranges, the range's unnormalised P V with the running max (log2 units) and the two
+// row sums.  m, l and le are the row's; l == 0 means no key was seen (a NaN passes on).
+//
+// The 8-bit cache's P V goes out in fp16, with the exponent of its scale: this rounds once more,
+// by at most 2^-11 of the value, an eighth of what P's rounding to bf16 may change, for half the
+// bytes of fp32.  The scale, a power of two, brings the row's largest magnitude to [2^14, 2^15),
+// the top of fp16's range, so that a column down to 2^-28 of it keeps all 11 bits.  Over pages
+// every 32 channels of a value have a scale of their own, so that columns may lie further apart
+// than that (and than 2^-39, where nothing would be left of the smaller ones): their P V stays
+// in fp32.
+template <int D, class F>
+__device__ __forceinline__ void store_rows(const typename F::Args& a, int64_t bh, int64_t row, int range,
                                            const f32x16 (&acc)[D / 32], float m, float l, float le, int hh) {
   float amax = 0.f;
-  if (a.ranges > 1) {
+  if (!F::PAGED && a.ranges > 1) {
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -87,21 +93,31 @@ __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, i
   if (row >= a.lq) return;
   const int64_t at = bh * a.lq + row;
   if (a.ranges > 1) {
-    int ex = 0;
-    if (amax > 0.f && amax <= 3.402823466e38f) ex = __builtin_amdgcn_frexp_expf(amax) - 15;
-    ex = ex < -126 ? -126 : ex;
-    const float sc = __builtin_amdgcn_ldexpf(1.0f, -ex);
     const int64_t prow = (int64_t)range * a.bh * a.lq + at;
-    _Float16* out = reinterpret_cast<_Float16*>(a.part_o) + prow * D + 4 * hh;
+    int ex = 0;
+    if constexpr (F::PAGED) {
+      float* out = reinterpret_cast<float*>(a.part_o) + prow * D + 4 * hh;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+      for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        f16x4 w;
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(out + 32 * t + 8 * g) =
+              make_float4(acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]);
+    } else {
+      if (amax > 0.f && amax <= 3.402823466e38f) ex = __builtin_amdgcn_frexp_expf(amax) - 15;
+      ex = ex < -126 ? -126 : ex;
+      const float sc = __builtin_amdgcn_ldexpf(1.0f, -ex);
+      _Float16* out = reinterpret_cast<_Float16*>(a.part_o) + prow * D + 4 * hh;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (_Float16)(acc[t][4 * g + e] * sc);
-        *reinterpret_cast<f16x4*>(out + 32 * t + 8 * g) = w;
-      }
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f16x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = (_Float16)(acc[t][4 * g + e] * sc);
+          *reinterpret_cast<f16x4*>(out + 32 * t + 8 * g) = w;
+        }
+    }
     if (hh == 0) reinterpret_cast<float4*>(a.part_meta)[prow] = make_float4(m, l, le, (float)ex);
     return;
   }
@@ -134,7 +150,10 @@ __device__ __forceinline__ void store_rows(const CacheAttnArgs& a, int64_t bh, i
 // spread evenly under them, K of tile t + 2 and V of tile t converted.  One barrier per
 // step, P MFMAs before its end, behind which the converted tiles can be read.
 // The softmax keeps a running max that is only refreshed when some lane's sum of a tile's
-// P exceeds 2^8 (attn_fwd.hip); the row sum of the bf16 P comes from 4x4x4 MFMAs.
+// P exceeds 2^8 (attn_fwd.hip); the row sum of the bf16 P comes from 4x4x4 MFMAs.  P is bf16
+// because its products' other operand, V, is: the scales of neither cache fit fp16's range.  A
+// weight is off by at most 2^-8 of itself and O by about as much as by its own rounding; P as
+// two bf16 numbers would make 24 products of a step's 16.
 //
 // D = 128, ms, all on one card (the clock differs between cards by some 3%):
 //                                          8 bits   4 bits   the bf16 forward
@@ -594,7 +613,7 @@ void cache_attn_kernel(typename F::Args a) {
       acc[m % C::DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           read_v(m, (ntiles - 1) % 2), pack_half(pp[m / C::DT / 2], m / C::DT % 2), acc[m % C::DT], 0, 0, 0);
   }
-  store_rows<D>(a, bh, row, range, acc, m_run, half_swap_sum(l_run), half_swap_sum(le_run), hh);
+  store_rows<D, F>(a, bh, row, range, acc, m_run, half_swap_sum(l_run), half_swap_sum(le_run), hh);
 }
 
 // Joins the ranges of one row: with M = max_r m_r and w_r = 2^(m_r - M),
@@ -614,14 +633,14 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(typename F::Args a) {
     // (four ranges' loads at once: with one after the other their latency was half of the time)
     for (int r0 = 0; r0 < a.ranges; r0 += 4 * G) {
       float4 x[4];
-      f16x8 u[4];
+      typename F::Part u[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] = make_float4(0.f, 0.f, 0.f, 0.f), u[i] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        x[i] = make_float4(0.f, 0.f, 0.f, 0.f), u[i] = typename F::Part{0, 0, 0, 0, 0, 0, 0, 0};
         if (r0 + i * G >= a.ranges) continue;
         const int64_t p = (int64_t)min(r0 + i * G + g, a.ranges - 1) * rows + row;
         x[i] = reinterpret_cast<const float4*>(a.part_meta)[p];
-        u[i] = *reinterpret_cast<const f16x8*>(reinterpret_cast<const _Float16*>(a.part_o) + p * D + 8 * c);
+        u[i] = reinterpret_cast<const typename F::Part*>(a.part_o)[p * LPR + c];
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {

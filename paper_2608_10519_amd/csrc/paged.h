@@ -66,7 +66,7 @@ struct PagedArgs {
 struct PagedAttnArgs : CacheAttnArgs {
   const int32_t* pages;            // [B, n_table]
   int64_t n_table, n_pages;
-  float* part32;                   // up to 32 rows: fp32 partial results [ranges, BH, Lq, D]
+  float* part32;                   // part_o, which holds fp32 here: unnormalised P V
   int waves, token_waves;          // of a work-group (launcher only), as in PagedPlan
   int join_groups;                 // (launcher only, more than 32 rows)
 };

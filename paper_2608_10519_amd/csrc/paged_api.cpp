@@ -182,9 +182,9 @@ static int paged_attn_common(const void* q, const void* k_pages, const void* v_p
   a.token_waves = plan.token_waves;
   a.join_groups = paged_join_groups(bh * Lq, D, plan.ranges);
   if (plan.ranges > 1) {
-    a.part_o = static_cast<uint16_t*>(workspace);  // (more than 32 rows)
     a.part32 = static_cast<float*>(workspace);
-    a.part_meta = reinterpret_cast<float*>(static_cast<char*>(workspace) + paged_part_bytes(bh * Lq, Lq, D, plan.ranges));
+    a.part_o = static_cast<uint16_t*>(workspace);
+    a.part_meta = reinterpret_cast<float*>(static_cast<char*>(workspace) + paged_part_bytes(bh * Lq, D, plan.ranges));
   }
   const hipError_t e = launch_paged_attn(a, D, dense, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return report_error(SPARSTAR_ERR_HIP, hipGetErrorString(e));

@@ -33,6 +33,10 @@ __device__ __forceinline__ uint32_t scale_byte(__amdgpu_buffer_rsrc_t rs, int at
 //     V's operand comes in that order from LDS: a lane loads 32 channels of a key, decodes
 //     them and stores them as bf16 rows, which the transpose read takes by columns.  A product
 //     with ones sums the rounded P.
+// P is rounded to bf16 because the products take both operands in one type and V has no other
+// of 16 bits: its scales reach far past fp16's range.  A weight is off by at most 2^-8 of itself,
+// O by about as much as by its own rounding to bf16 (0.0017 of it, 0.0024 with both); P as a sum
+// of two bf16 numbers would double the products of P V.
 template <int D, int NC, bool DENSE, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_token_kernel(PagedAttnArgs a) {

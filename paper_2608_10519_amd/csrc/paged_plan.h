@@ -19,10 +19,12 @@ inline int paged_token_most_ranges(int64_t bh, int64_t lk, int block) {
 }
 
 // The same of more rows: the 8-bit cache's, and as many as fill the chip three times with a wave
-// per 32 rows, of 64 keys at least.
+// per 32 rows, of 64 keys at least.  From 2^18 rows of all heads on no cut has more than eight
+// (of 300,000 random sizes): more would only ask for a larger workspace.
 inline int paged_rows_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block) {
   const int64_t waves = bh * ((lq + 31) / 32), filled = 3 * 256 * 4 * kAttnWavesPerSimd / std::max<int64_t>(waves, 1);
-  return (int)std::max<int64_t>(cache_attn_most_ranges(bh, lq, lk, block), std::min<int64_t>({filled, (lk + 63) / 64, 64}));
+  const int64_t most = std::max<int64_t>(cache_attn_most_ranges(bh, lq, lk, block), std::min<int64_t>({filled, (lk + 63) / 64, 64}));
+  return (int)std::min<int64_t>(most, bh * lq >= 1 << 18 ? 8 : 64);
 }
 
 // The time of a call of more than 32 rows whose lists hold `keys` keys, us: its start, the tiles
@@ -30,8 +32,11 @@ inline int paged_rows_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block)
 // round after round, and the join.  (Work-groups without work take places too: the last round of
 // two heads of 2,325 rows in 13 ranges starts 8 of 520, 49 us; in 12 ranges 39.)  Fitted to 450
 // random shapes of up to 250 us (1 to 72 heads, 33 to 6,000 x 200 to 140,000, dense and 5% to 65%,
-// both head dims and block sizes), each timed at some 13 cuts; on 500 others the cut of the least
-// estimate is 0.8% slower than the best one on average, the 8-bit cache's cut 7% (up to 97%).
+// both head dims and block sizes), each timed at some 13 cuts, and the join's terms again, for
+// results in fp32, to 300 such.  On 200 others the cut of the least estimate is 0.8% slower than
+// the best one on average (the 8-bit cache's cut was 7%, up to 97%).  It ranks cuts and is no
+// prediction: nine cuts in ten above 14 us take 0.83 to 1.06 times what it says, and lists
+// that cluster up to a third more.
 inline double paged_rows_time_us(int64_t bh, int64_t lq, int64_t keys, int d, int ranges, int rows) {
   static constexpr double kTileUs[2][2][4] = {{{.82, 1.17, 1.23, 1.32}, {.78, 1.18}}, {{.71, .95, 1.01, 1.09}, {.66, .95}}};
   static constexpr double kStart[2][2] = {{.94, 1.3}, {.64, 1.7}};  // tiles that a work-group's start costs
@@ -43,7 +48,7 @@ inline double paged_rows_time_us(int64_t bh, int64_t lq, int64_t keys, int d, in
   const double tiles = double(keys) / ranges / attn_tile_keys(d) + kStart[d == 128][rows == 128];
   double t = 5.6 + double(whole) * tiles * us[per_cu - 1];
   if (part > 0) t += tiles * us[(part + 31) / 32 - 1];
-  if (ranges > 1) t += 4.7 + 0.02 * ranges + double(bh) * double(lq) * ranges * (2 * d + 16) / 1.7e6;
+  if (ranges > 1) t += 4.2 + 0.06 * ranges + double(bh) * double(lq) * ranges * (4 * d + 16) / 2.6e6;
   return t;
 }
 
@@ -71,10 +76,12 @@ inline CachePlan paged_rows_plan(int64_t bh, int64_t lq, int64_t lk, int d, int 
   }
   if (p.ranges == 0) {
     p = cache_attn_plan(bh, lq, lk, d, block, kv_stride, dense, may_split);
+    p.ranges = std::min(p.ranges, most);
     const bool full = dense || kv_stride >= nk;
     const double rho = full ? 1.0 : double(kv_stride) / double(nk);
-    auto time = [&](int ranges, int rows) {
-      return attn_time_us(bh, lq, lk, d, block, rho, full, ranges, p.rotation > 0, rows);
+    auto time = [&](int ranges, int rows) {  // (with the ranges' results in fp32, not fp16)
+      return attn_time_us(bh, lq, lk, d, block, rho, full, ranges, p.rotation > 0, rows) +
+             (ranges > 1 ? double(bh) * double(lq) * ranges * 4 * d / 6.3e6 : 0.0);
     };
     best = 0.98 * time(p.ranges, 32 * p.waves);
     int ranges = p.ranges, rows = 32 * p.waves;
@@ -133,19 +140,19 @@ inline PagedPlan paged_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int 
   return p;
 }
 
-// Bytes of workspace: the ranges' results, fp32 for up to 32 rows, and four values per row.
-inline size_t paged_part_bytes(int64_t rows, int64_t lq, int d, int ranges) {
-  return lq > 32 ? cache_part_o_bytes(rows, d, ranges) : (size_t(rows * d) * ranges * 4 + 255) & ~size_t(255);
+// Bytes of workspace: the ranges' results in fp32, and four values per row.
+inline size_t paged_part_bytes(int64_t rows, int d, int ranges) {
+  return (size_t(rows * d) * ranges * 4 + 255) & ~size_t(255);
 }
 inline size_t paged_attn_workspace(int64_t bh, int64_t lq, int64_t lk, int d, int block) {
   const int ranges = lq > 32 ? paged_rows_most_ranges(bh, lq, lk, block) : paged_token_most_ranges(bh, lk, block);
-  return ranges > 1 ? paged_part_bytes(bh * lq, lq, d, ranges) + size_t(bh * lq) * ranges * 4 * sizeof(float) : 0;
+  return ranges > 1 ? paged_part_bytes(bh * lq, d, ranges) + size_t(bh * lq) * ranges * 4 * sizeof(float) : 0;
 }
 
 // Groups of threads that share the join of a row's ranges (cache_merge_kernel; a thread loads four
-// ranges at a time).  D = 128, us in one, 4 and 16 groups: 64 rows in 16 ranges 5.2, 3.9, 3.9, in 64
-// 16.5, 6.4, 4.0; 2,400 in 8 3.9, 4.0, 5.1, in 16 5.5, 4.6, 6.0, in 64 16.9, 9.1, 11.4; 7,200 in 16
-// 7.4, 7.8, 12.3, in 64 21.6, 21.8, 27.5.
+// ranges at a time).  D = 128, us in one, 4 and 16 groups: 64 rows in 16 ranges 6.3, 4.0, 4.0, in 64
+// 20.6, 7.5, 4.0; 2,400 in 8 4.8, 4.7, 5.2, in 16 7.2, 5.4, 6.4, in 32 12.4, 8.3, 9.9; 7,200 in 8
+// 6.6, 6.8, 10.2, in 12 8.5, 8.6, 11.4.
 inline int paged_join_groups(int64_t rows, int d, int ranges) {
   if (ranges <= 8 || rows * d >= 5000 * 128) return 1;
   return ranges > 16 && rows * d <= 1000 * 128 ? 16 : 4;
