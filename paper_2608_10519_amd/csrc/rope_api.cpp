@@ -43,8 +43,8 @@ int check_turn(const float* table, int64_t table_rows, int pairs, int interleave
                int64_t start, int64_t L, bool anywhere, Turn* out) {
   if (pairs < 8 || pairs % 8 != 0 || pairs > D / 2)
     return report_error(SPARSTAR_ERR_INVALID_ARG, "pairs must be a multiple of 8 in [8, D / 2]");
-  if (table_rows < 1 || table_rows > (int64_t(1) << 40))
-    return report_error(SPARSTAR_ERR_INVALID_ARG, "table_rows must be in [1, 2^40]");
+  if (table_rows < (L > 0) || table_rows > (int64_t(1) << 40))
+    return report_error(SPARSTAR_ERR_INVALID_ARG, "table_rows must be in [1, 2^40], or 0 without tokens");
   if (reinterpret_cast<uintptr_t>(table) & 15u)
     return report_error(SPARSTAR_ERR_INVALID_ARG, "the table must be 16-byte aligned");
   if (reinterpret_cast<uintptr_t>(positions) & 3u)
