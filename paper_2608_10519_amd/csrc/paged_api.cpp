@@ -107,6 +107,13 @@ extern "C" size_t sparstar_paged_attn_workspace_bytes(int B, int H, int64_t Lq, 
   return paged_attn_workspace(int64_t(B) * H, Lq, Lk, D, block_size);
 }
 
+// The cut of a call of more than 32 rows with a workspace; kv_stride 0: dense.
+extern "C" void sparstar_internal_paged_plan(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
+                                             int64_t kv_stride, int64_t* out) {
+  const CachePlan p = paged_rows_plan(int64_t(B) * H, Lq, Lk, D, block_size, kv_stride, kv_stride == 0, true);
+  out[0] = p.waves, out[1] = p.ranges, out[2] = p.rotation;
+}
+
 extern "C" int sparstar_internal_paged_ranges(int B, int H, int64_t Lq, int64_t Lk, int D, int block_size,
                                               int64_t kv_stride) {
   if (check_attn_sizes(B, H, Lq, Lk, D, block_size) != SPARSTAR_OK) return 1;
