@@ -39,7 +39,6 @@ struct Codes8 {
   using Args = CacheAttnArgs;
   using Part = f16x8;  // of a range's P V (store_rows)
   static constexpr bool PAGED = false;
-  static constexpr int BITS = 8;
   struct Piece {
     uint4 u;
   };
@@ -51,7 +50,6 @@ struct Codes4 {
   using Args = PagedAttnArgs;
   using Part = f32x8;
   static constexpr bool PAGED = true;
-  static constexpr int BITS = 4;
   struct Piece {
     uint2 u;
     uint32_t s;
