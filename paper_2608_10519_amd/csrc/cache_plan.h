@@ -67,8 +67,10 @@ inline CachePlan cache_attn_plan(int64_t bh, int64_t lq, int64_t lk, int d, int 
   return c;
 }
 
-// Groups of threads that share the join of a row's ranges (cache_merge_kernel): a group per D / 8
-// threads reads a range at a time, few rows fill the chip with 16 of them.
+// Groups of threads that share the join of a row's ranges (cache_merge_kernel).  A group of D / 8
+// threads loads four ranges at a time; few rows fill the chip with 16 of them.  Fewer would be
+// faster between (2,400 rows in 8 ranges 5.1 us with 16 groups, 3.9 with one), but the groups are
+// the order in which ranges are added, and results keep their last bits.
 inline int cache_join_groups(int waves, int64_t rows, int ranges) {
   return waves == 1 || rows <= 4096 || ranges > kSplits ? 16 : 1;
 }
