@@ -153,15 +153,16 @@ __device__ __forceinline__ void store_rows(const typename F::Args& a, int64_t bh
 // weight is off by at most 2^-8 of itself and O by about as much as by its own rounding; P as
 // two bf16 numbers would make 24 products of a step's 16.
 //
-// D = 128, ms, all on one card (the clock differs between cards by some 3%):
+// D = 128, N(0, 1) and random lists, ms, all on one card (the clock differs between cards by
+// some 3%, and with the data: what needs fewer bits takes less power):
 //                                          8 bits   4 bits   the bf16 forward
-//   24 heads,  2,880 x  75,392, dense       2.69     2.62     2.58
-//   24 heads, 25,920 x  98,432, dense      29.5     29.2     28.4
-//   24 heads, 11,520 x  84,032, 25%         3.45     3.34     3.25
-//   24 heads, 72,000 x 144,512, 25%        34.9     34.3     33.7
-//   24 heads, 72,000 x 144,512, 9.4%, 128  13.0     12.7     13.5
-//    8 heads, 11,520 x  84,032, 25%         1.18     1.16     1.13
-//    8 heads, 11,520 x  84,032, 25%, 128    1.05     1.02     1.03
+//   24 heads,  2,880 x  75,392, dense       2.66     2.60     2.56
+//   24 heads, 25,920 x  98,432, dense      29.4     29.4     28.0
+//   24 heads, 11,520 x  84,032, 25%         3.49     3.48     3.17
+//   24 heads, 72,000 x 144,512, 25%        34.8     35.0     33.6
+//   24 heads, 72,000 x 144,512, 9.4%, 128  12.6     12.9     12.7
+//    8 heads, 11,520 x  84,032, 25%         1.23     1.20     1.11
+//    8 heads, 11,520 x  84,032, 25%, 128    1.08     1.05     1.02
 // The first is 1.02 PFLOP/s with 4 bits, the matrix cores busy half of the cycles at 1.8 GHz, the
 // VALU issuing 0.10 instructions per SIMD and cycle.
 template <int D, int NW>

@@ -30,7 +30,7 @@ inline int paged_rows_most_ranges(int64_t bh, int64_t lq, int64_t lk, int block)
 // The time of a call of more than 32 rows whose lists hold `keys` keys, us: its start, the tiles
 // of work-groups that a CU holds one, two, three or four of (of two waves; of four: one or two),
 // round after round, and the join.  (Work-groups without work take places too: the last round of
-// two heads of 2,325 rows in 13 ranges starts 8 of 520, 49 us; in 12 ranges 39.)  Fitted to 450
+// two heads of 2,325 x 14,000, D = 64, in 13 ranges starts 8 of 520, 45 us; in 12 ranges 37.5.)  Fitted to 450
 // random shapes of up to 250 us (1 to 72 heads, 33 to 6,000 x 200 to 140,000, dense and 5% to 65%,
 // both head dims and block sizes), each timed at some 13 cuts, and the join's terms again, for
 // results in fp32, to 300 such.  On 200 others the cut of the least estimate is 0.8% slower than
@@ -53,9 +53,9 @@ inline double paged_rows_time_us(int64_t bh, int64_t lq, int64_t keys, int d, in
 }
 
 // More than 32 rows take the cut of the least estimated time, among some numbers of ranges and
-// those that fill the chip once, twice or three times: 24 heads of 64 x 144,512 183 us in 32
-// ranges, 168 in 42; one head of 719 x 771 25 us whole, 12.5 in 12; 50 heads of 157 rows with lists of
-// 2,048 keys 52 us whole, 32 in 5.  Calls of more than 300 us, where the lists' shares of the L2
+// those that fill the chip once, twice or three times: 24 heads of 64 x 144,512 203 us in 32
+// ranges, 173 in 42; one head of 719 x 771 22 us whole, 13.4 in 8; 50 heads of 157 rows with lists of
+// 2,048 keys 53 us whole, 31 in 6.  Calls of more than 300 us, where the lists' shares of the L2
 // count, take the 8-bit cache's cut, or a number of ranges that fills the chip where the forward's
 // estimate finds that faster by 2%: 24 heads of 2,880 x 75,392 six ranges.
 inline CachePlan paged_rows_plan(int64_t bh, int64_t lq, int64_t lk, int d, int block, int64_t kv_stride, bool dense,
