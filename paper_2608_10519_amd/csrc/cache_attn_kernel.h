@@ -31,6 +31,8 @@ __device__ __forceinline__ bf16x8 decode8(uint2 u, float scale) {
   return __builtin_bit_cast(bf16x8, r);
 }
 
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
 // The two kinds of cache.  A lane takes 16 codes of a tile at a time (a piece), and turns
 // them into two chunks of eight bf16 values.
 //
